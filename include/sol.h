@@ -306,6 +306,80 @@ sol_status_t sol_kv_refresh(const sol_shape_t *shape, int32_t n_layers, const so
                             const sol_kv_t *kvs, int32_t B, int32_t n_tokens, const void *h_in_bf16,
                             void *h_out_bf16, void *ws, size_t ws_bytes, sol_stream_t stream);
 
+/* ---- speculative decoding: a tree of drafted tokens per sequence, verified in one pass ----
+ * (the paper has no counterpart; a serving loop needs it next to the decode step)
+ *
+ * The drafted nodes of sequence b are the last n_nodes[b] tokens of its cache: slots T_b - n_nodes[b] .. T_b - 1 hold
+ * their keys and values in node order, seq_lens counts them, the tokens before them are the committed context.
+ * At most 64 nodes; trees of a batch may differ, also in size.  A count outside 0 .. max_nodes, or above the
+ * sequence's length, raises the bad-action bit of the device status word and is clamped. */
+#define SOL_MAX_TREE_NODES 64
+typedef struct sol_tree {
+  int32_t max_nodes;      /* 1..64: rows per sequence of every [B][max_nodes] array */
+  const int32_t *n_nodes; /* device [B] */
+  const uint64_t *mask;   /* device [B][max_nodes]: bit j of node i's word: i attends to node j.  Whatever the caller
+                             puts there counts (a chain's lower triangle, a tree's ancestors, a node without itself);
+                             bits of nodes that are not there are ignored */
+} sol_tree_t;
+/* Ancestor masks (the node itself among them) and, optionally, depths (a root's is 0) of trees given by their parents:
+ * parents[b][i] < i, or -1 for a root; any other value counts as -1.  Rows behind a tree's last node are left as they
+ * were, here and in every call below.  Any batch size; needs no workspace.
+ *   n_nodes [B]; parents [B][max_nodes]; mask [B][max_nodes] out; depth [B][max_nodes] out, optional. */
+sol_status_t sol_tree_build(int32_t B, int32_t max_nodes, const int32_t *n_nodes, const int32_t *parents, uint64_t *mask,
+                            int32_t *depth, sol_stream_t stream);
+/* Scratch of sol_tree_attn for batches up to max_batch (it depends on the device's SM count: ask on the device that runs
+ * the call); sol_workspace_init as for the other workspaces.  0: unsupported. */
+size_t sol_tree_workspace_bytes(const sol_shape_t *shape, int32_t max_batch, int32_t max_pages_per_seq, int32_t max_nodes);
+/* Attention of the drafted nodes over the cache: node i attends to all of the committed context and to the nodes its mask
+ * names, softmax over those; a node that sees nothing (no context, empty mask) gets zeros.  Keep-rates, sinks, windows and
+ * the page selection do not act here.  What a masked node's key and value hold, numbers or not, does not reach a row that
+ * does not see it; neither do slots behind the sequence.  Tokens of a page whose number is out of range are skipped and
+ * raise the status bit.  At most 256 kv-heads.
+ *   q_bf16 [B][max_nodes][n_q][head_dim] (already rotated); out_bf16 the same shape. */
+sol_status_t sol_tree_attn(const sol_shape_t *shape, const void *q_bf16, const sol_kv_t *kv, const sol_tree_t *tree, int32_t B,
+                           void *out_bf16, void *ws, size_t ws_bytes, sol_stream_t stream);
+/* The path of a tree that the model's own tokens accept: it starts at node 0 (the token the last step ended with) and goes
+ * on to the child with the lowest index whose drafted token is target_tokens of the current node (the token the model puts
+ * after it), until there is none.  Any batch size; needs no workspace.
+ *   draft_tokens, target_tokens [B][max_nodes]; path [B][max_nodes] out: the accepted nodes, ascending; path_len [B] out
+ *   (0 for an empty tree); next_token [B] out, optional: target_tokens of the last accepted node (-1 for an empty tree). */
+sol_status_t sol_tree_accept(int32_t B, int32_t max_nodes, const int32_t *n_nodes, const int32_t *parents,
+                             const int32_t *draft_tokens, const int32_t *target_tokens, int32_t *path, int32_t *path_len,
+                             int32_t *next_token, sol_stream_t stream);
+/* Commits a path in all layers: the keys and values of its j-th node move to slot T_b - n_nodes[b] + j, in place; the other
+ * nodes' slots are then free.  (A node of depth j was rotated for that position.)  The path must ascend; it ends at the
+ * first entry that does not, or that is no node, which raises the bad-action bit.
+ *   kvs: HOST array of n_layers structs; tree: n_nodes and max_nodes (the mask may be NULL); new_lens [B] out, optional:
+ *   the lengths of kvs[0] afterwards; it must not overlap any seq_lens; ws: an initialised workspace of any size (its
+ *   status words). */
+sol_status_t sol_tree_commit(const sol_shape_t *shape, int32_t n_layers, const sol_kv_t *kvs, const sol_tree_t *tree, int32_t B,
+                             const int32_t *path, const int32_t *path_len, int32_t *new_lens, void *ws, sol_stream_t stream);
+
+/* ---- a bounded cache: attention that adds up what each cached token receives, and eviction by it ----
+ * Dense decode attention of one query token per sequence (the newest, seq_lens counts it) over its whole cache, and
+ *   weights[b][h][t] = decay * weights[b][h][t] + sum over the query heads of kv-head h of their softmax weight on token t
+ * for every token t of the sequence; the newest token's entry is set to this step's sum.  Entries behind a sequence are left
+ * as they were.  An empty sequence gets zeros.  Keep-rates, sinks, windows and the page selection do not act here.
+ *   q_bf16, out_bf16 [B][n_q][head_dim]; weights float32 [B][n_kv][max_pages_per_seq * page_size]; 0 <= decay <= 1;
+ *   ws: sol_workspace_bytes.  At most 256 kv-heads. */
+sol_status_t sol_weighted_decode_attn(const sol_shape_t *shape, const void *q_bf16, const sol_kv_t *kv, int32_t B, float decay,
+                                      float *weights, void *out_bf16, void *ws, size_t ws_bytes, sol_stream_t stream);
+/* Eviction: of every (sequence, kv-head) min(T, max(budgets[b], forced)) tokens stay: the first shape->n_sink, the last
+ * shape->n_window, and of the others those with the largest weight (ties: lower index; a weight that is no number counts
+ * less than any).  They move together, in order, to slots 0, 1, ... of the pages in dst_table, their weights to
+ * dst_weights; what lies behind them is left as it was.  With shape->rope_theta a key that moves from slot i to slot j is
+ * rotated by j - i positions (in float32, rounded to bf16), so that every slot t holds a key at position t, as
+ * sol_decode_layer expects of the cache it appends to; without it keys are copied.
+ *   budgets [B]; weights, dst_weights float32 [B][n_kv][max_pages_per_seq * page_size]; dst_table int32
+ *   [B][max_pages_per_seq], of the same pools; dst_lens [B] out: the new lengths; it must not overlap kv->seq_lens;
+ *   kept_idx (optional) int32 [B][n_kv][max_pages_per_seq * page_size] out: the kept tokens' old slots, ascending.
+ * In place: dst_table may be kv->page_table (or hold the same pages in the same places) and dst_weights may be weights.
+ * Otherwise the destinations must not overlap what any sequence of the batch still reads.  The Quest extrema are not updated:
+ * call sol_quest_build_meta afterwards.  ws: sol_workspace_bytes.  At most 256 kv-heads. */
+sol_status_t sol_kv_evict(const sol_shape_t *shape, const sol_kv_t *kv, int32_t B, const int32_t *budgets, const float *weights,
+                          const int32_t *dst_table, float *dst_weights, int32_t *dst_lens, int32_t *kept_idx, void *ws,
+                          size_t ws_bytes, sol_stream_t stream);
+
 /* The same step for a caller whose per-step data lives on the HOST: h_in,
  * the three action arrays, seq_lens and h_out are host pointers (pinned
  * memory makes the copies of h_in and h_out asynchronous; the four int32

@@ -26,7 +26,8 @@ EXPORTS = [
     "sol_packed_weight_bytes", "sol_pack_weights", "sol_quant_act_wide", "sol_quest_meta_bytes", "sol_quest_build_meta",
     "sol_sparse_decode_attn", "sol_sparse_decode_attn_static", "sol_pruned_swiglu_mlp", "sol_decode_layer", "sol_decode_step",
     "sol_decode_step_traced", "sol_kv_refresh", "sol_decode_step_host", "sol_read_device_status", "sol_selftest_wait_timeout", "sol_timing_enable", "sol_timing_collect",
-    "sol_launch_count",
+    "sol_launch_count", "sol_tree_workspace_bytes", "sol_tree_build", "sol_tree_attn", "sol_tree_accept", "sol_tree_commit",
+    "sol_weighted_decode_attn", "sol_kv_evict",
 ]
 
 
@@ -42,6 +43,10 @@ class SolKV(C.Structure):
     _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("page_table", C.c_void_p),
                 ("seq_lens", C.c_void_p), ("max_pages_per_seq", C.c_int32), ("num_pages", C.c_int32),
                 ("quest_meta", C.c_void_p)]
+
+
+class SolTree(C.Structure):
+    _fields_ = [("max_nodes", C.c_int32), ("n_nodes", C.c_void_p), ("mask", C.c_void_p)]
 
 
 class SolLayerWeights(C.Structure):
@@ -123,6 +128,20 @@ def lib() -> C.CDLL:
                                            P, P, P, P, P, P, P, S, P]
         L.sol_read_device_status.restype = I
         L.sol_read_device_status.argtypes = [P, C.POINTER(C.c_int32), P]
+        L.sol_tree_workspace_bytes.restype = S
+        L.sol_tree_workspace_bytes.argtypes = [C.POINTER(SolShape), I, I, I]
+        L.sol_tree_build.restype = I
+        L.sol_tree_build.argtypes = [I, I, P, P, P, P, P]
+        L.sol_tree_attn.restype = I
+        L.sol_tree_attn.argtypes = [C.POINTER(SolShape), P, C.POINTER(SolKV), C.POINTER(SolTree), I, P, P, S, P]
+        L.sol_tree_accept.restype = I
+        L.sol_tree_accept.argtypes = [I, I, P, P, P, P, P, P, P, P]
+        L.sol_tree_commit.restype = I
+        L.sol_tree_commit.argtypes = [C.POINTER(SolShape), I, C.POINTER(SolKV), C.POINTER(SolTree), I, P, P, P, P, P]
+        L.sol_weighted_decode_attn.restype = I
+        L.sol_weighted_decode_attn.argtypes = [C.POINTER(SolShape), P, C.POINTER(SolKV), I, C.c_float, P, P, P, S, P]
+        L.sol_kv_evict.restype = I
+        L.sol_kv_evict.argtypes = [C.POINTER(SolShape), C.POINTER(SolKV), I, P, P, P, P, P, P, P, S, P]
         L.sol_timing_enable.restype = None
         L.sol_timing_enable.argtypes = [I]
         L.sol_timing_collect.restype = I
@@ -319,6 +338,74 @@ def kv_refresh(shape, layers, kvs, B: int, n_tokens: int, h_in_bf16, h_out_bf16,
                              _ptr(ws), ws_bytes, _stream(stream))
     if check:
         _check(s, "sol_kv_refresh")
+    return s
+
+
+MAX_TREE_NODES = 64
+
+
+def make_tree(max_nodes: int, n_nodes, mask=None) -> SolTree:
+    """Trees of drafted tokens: n_nodes int32 [B], mask 64-bit words [B][max_nodes] (tree_commit needs none)."""
+    return SolTree(max_nodes, _ptr(n_nodes), _ptr(mask))
+
+
+def tree_workspace_bytes(shape: SolShape, max_batch: int, max_pages_per_seq: int, max_nodes: int) -> int:
+    return int(lib().sol_tree_workspace_bytes(C.byref(shape), max_batch, max_pages_per_seq, max_nodes))
+
+
+def tree_build(B: int, max_nodes: int, n_nodes, parents, mask, depth=None, stream=None, check=True) -> int:
+    """Ancestor masks and depths of the trees that `parents` describes."""
+    s = lib().sol_tree_build(B, max_nodes, _ptr(n_nodes), _ptr(parents), _ptr(mask), _ptr(depth), _stream(stream))
+    if check:
+        _check(s, "sol_tree_build")
+    return s
+
+
+def tree_attn(shape, q_bf16, kv: SolKV, tree: SolTree, B: int, out_bf16, ws, ws_bytes: int, stream=None, check=True) -> int:
+    s = lib().sol_tree_attn(C.byref(shape), _ptr(q_bf16), C.byref(kv), C.byref(tree), B, _ptr(out_bf16), _ptr(ws), ws_bytes,
+                            _stream(stream))
+    if check:
+        _check(s, "sol_tree_attn")
+    return s
+
+
+def tree_accept(B: int, max_nodes: int, n_nodes, parents, draft_tokens, target_tokens, path, path_len, next_token=None,
+                stream=None, check=True) -> int:
+    """The path that the model's own tokens accept."""
+    s = lib().sol_tree_accept(B, max_nodes, _ptr(n_nodes), _ptr(parents), _ptr(draft_tokens), _ptr(target_tokens), _ptr(path),
+                              _ptr(path_len), _ptr(next_token), _stream(stream))
+    if check:
+        _check(s, "sol_tree_accept")
+    return s
+
+
+def tree_commit(shape, kvs: Sequence[SolKV], tree: SolTree, B: int, path, path_len, new_lens, ws, stream=None,
+                check=True) -> int:
+    """Moves an accepted path's keys and values to the end of the committed context, in every layer of `kvs`."""
+    s = lib().sol_tree_commit(C.byref(shape), len(kvs), (SolKV * len(kvs))(*kvs), C.byref(tree), B, _ptr(path),
+                              _ptr(path_len), _ptr(new_lens), _ptr(ws), _stream(stream))
+    if check:
+        _check(s, "sol_tree_commit")
+    return s
+
+
+def weighted_decode_attn(shape, q_bf16, kv: SolKV, B: int, decay: float, weights, out_bf16, ws, ws_bytes: int, stream=None,
+                         check=True) -> int:
+    """Dense decode attention that also adds up the attention weight of every cached token."""
+    s = lib().sol_weighted_decode_attn(C.byref(shape), _ptr(q_bf16), C.byref(kv), B, decay, _ptr(weights), _ptr(out_bf16),
+                                       _ptr(ws), ws_bytes, _stream(stream))
+    if check:
+        _check(s, "sol_weighted_decode_attn")
+    return s
+
+
+def kv_evict(shape, kv: SolKV, B: int, budgets, weights, dst_table, dst_weights, dst_lens, kept_idx, ws, ws_bytes: int,
+             stream=None, check=True) -> int:
+    """Keeps the budget's tokens of largest weight per (sequence, kv-head); dst_table and dst_weights may be the cache's own."""
+    s = lib().sol_kv_evict(C.byref(shape), C.byref(kv), B, _ptr(budgets), _ptr(weights), _ptr(dst_table), _ptr(dst_weights),
+                           _ptr(dst_lens), _ptr(kept_idx), _ptr(ws), ws_bytes, _stream(stream))
+    if check:
+        _check(s, "sol_kv_evict")
     return s
 
 

@@ -1,5 +1,7 @@
 // C ABI of the library: argument validation, workspace layout, and the
 // composition of the kernels into attention, MLP, layer and step calls.
+#include <cuda.h>
+
 #include <atomic>
 #include <cstdio>
 #include <cstring>
@@ -92,6 +94,34 @@ void ensure_dynamic_smem(const void* kernel, int bytes) {
 // ---------------------------------------------------------------------------
 // workspace layout
 // ---------------------------------------------------------------------------
+bool encode_pool_map(CUtensorMap* map, const void* pool, const sol_shape_t& sh, int num_pages, int box_rows) {
+  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static std::atomic<void*> found{nullptr};
+  void* fn = found.load(std::memory_order_acquire);
+  if (!fn) {
+    cudaDriverEntryPointQueryResult q;
+    if (record_cuda_error(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q),
+                          "cuTensorMapEncodeTiled"))
+      return false;
+    if (!fn) {
+      record_cuda_error(cudaErrorNotSupported, "cuTensorMapEncodeTiled");
+      return false;
+    }
+    found.store(fn, std::memory_order_release);
+  }
+  const cuuint64_t dims[2] = {(cuuint64_t)sh.head_dim, (cuuint64_t)num_pages * sh.n_kv_heads * PAGE};
+  const cuuint64_t strides[1] = {(cuuint64_t)sh.head_dim * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, step[2] = {1, 1};
+  const CUresult r = reinterpret_cast<Encode>(fn)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(pool), dims, strides,
+                                                  box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r == CUDA_SUCCESS) return true;
+  record_cuda_error(cudaErrorInvalidValue, "tensor map of a cache pool");
+  return false;
+}
+
 struct Layout {
   size_t status, zero_p, stage_h_in, stage_act, stage_h_out, a_op, scale, qkv, attn_hi, attn_lo, attn_f32, h_mid, o_part, g, u, t, t_hi, t_lo, kept_ch_cnt, live, ch_sel, ch_cand_val, ch_cand_idx, ch_keep, down_part,
       h_a, h_b, refresh_tab, refresh_act, total;
@@ -749,6 +779,121 @@ sol_status_t sol_kv_refresh(const sol_shape_t* shape, int32_t n_layers, const so
       }
     }
   }
+  return finish();
+}
+
+// ---------------------------------------------------------------------------
+// speculative decoding and a bounded cache
+// ---------------------------------------------------------------------------
+// What the dense attention calls ask of a shape and a cache beyond shape_ok and kv_ok: the line of tiles is counted in 32 bits,
+// and tensor maps take pools on 16-byte boundaries with row numbers below 2^31.
+static bool aligned16(const void* a) { return (reinterpret_cast<uintptr_t>(a) & 15) == 0; }
+static bool cache_size_ok(const sol_shape_t* s, const sol_kv_t* kv) {
+  return s->n_kv_heads <= 256 && kv->max_pages_per_seq <= MAX_PAGES_PER_SEQ &&
+         (long long)kv->num_pages * s->n_kv_heads * PAGE < (1ll << 31);
+}
+static bool tree_ok(const sol_tree_t* t) { return t && t->n_nodes && t->mask && t->max_nodes >= 1; }
+
+size_t sol_tree_workspace_bytes(const sol_shape_t* shape, int32_t max_batch, int32_t max_pages_per_seq, int32_t max_nodes) {
+  if (!shape_ok(shape) || max_batch < 1 || max_batch > 128 || max_pages_per_seq < 1 || max_pages_per_seq > MAX_PAGES_PER_SEQ ||
+      max_nodes < 1 || max_nodes > MAX_TREE_NODES || shape->n_kv_heads > 256)
+    return 0;
+  return 256 + rows_part_bytes(*shape);
+}
+
+sol_status_t sol_tree_build(int32_t B, int32_t max_nodes, const int32_t* n_nodes, const int32_t* parents, uint64_t* mask,
+                            int32_t* depth, sol_stream_t stream) {
+  if (!n_nodes || !parents || !mask || B < 0 || max_nodes < 1) return SOL_ERR_INVALID_ARG;
+  if (max_nodes > MAX_TREE_NODES) return SOL_ERR_UNSUPPORTED;
+  if (B == 0) return SOL_OK;
+  launch_tree_build(B, max_nodes, n_nodes, parents, mask, depth, (cudaStream_t)stream);
+  return finish();
+}
+
+sol_status_t sol_tree_attn(const sol_shape_t* shape, const void* q_bf16, const sol_kv_t* kv, const sol_tree_t* tree, int32_t B,
+                           void* out_bf16, void* ws, size_t ws_bytes, sol_stream_t stream) {
+  if (!shape || !q_bf16 || !kv_ok(kv) || !tree_ok(tree) || !out_bf16 || !ws || B < 0) return SOL_ERR_INVALID_ARG;
+  if (!aligned16(q_bf16) || !aligned16(out_bf16) || !aligned16(kv->k_pool) || !aligned16(kv->v_pool) || !aligned16(ws))
+    return SOL_ERR_INVALID_ARG;
+  if (!shape_ok(shape) || B > 128 || !cache_size_ok(shape, kv) || tree->max_nodes > MAX_TREE_NODES) return SOL_ERR_UNSUPPORTED;
+  if (B == 0) return SOL_OK;
+  if (ws_bytes < sol_tree_workspace_bytes(shape, B, kv->max_pages_per_seq, tree->max_nodes)) return SOL_ERR_WORKSPACE_TOO_SMALL;
+  RowsArgs a;
+  memset(&a, 0, sizeof(a));
+  a.shape = *shape; a.kv = *kv; a.B = B;
+  a.max_nodes = tree->max_nodes; a.n_nodes = tree->n_nodes; a.mask = tree->mask;
+  a.q = q_bf16; a.out = out_bf16;
+  a.part = at<float>(ws, 256); a.part_bytes = rows_part_bytes(*shape);
+  a.status = at<int>(ws, 0);
+  launch_rows_attention(a, (cudaStream_t)stream);
+  return finish();
+}
+
+sol_status_t sol_tree_accept(int32_t B, int32_t max_nodes, const int32_t* n_nodes, const int32_t* parents,
+                             const int32_t* draft_tokens, const int32_t* target_tokens, int32_t* path, int32_t* path_len,
+                             int32_t* next_token, sol_stream_t stream) {
+  if (!n_nodes || !parents || !draft_tokens || !target_tokens || !path || !path_len || B < 0 || max_nodes < 1)
+    return SOL_ERR_INVALID_ARG;
+  if (max_nodes > MAX_TREE_NODES) return SOL_ERR_UNSUPPORTED;
+  if (B == 0) return SOL_OK;
+  launch_tree_accept(B, max_nodes, n_nodes, parents, draft_tokens, target_tokens, path, path_len, next_token, (cudaStream_t)stream);
+  return finish();
+}
+
+sol_status_t sol_tree_commit(const sol_shape_t* shape, int32_t n_layers, const sol_kv_t* kvs, const sol_tree_t* tree, int32_t B,
+                             const int32_t* path, const int32_t* path_len, int32_t* new_lens, void* ws, sol_stream_t stream) {
+  if (!shape || n_layers < 1 || !kvs || !tree || !tree->n_nodes || tree->max_nodes < 1 || !path || !path_len || !ws || B < 0)
+    return SOL_ERR_INVALID_ARG;
+  for (int l = 0; l < n_layers; ++l)
+    if (!kv_ok(&kvs[l]) || !aligned16(kvs[l].k_pool) || !aligned16(kvs[l].v_pool)) return SOL_ERR_INVALID_ARG;
+  if (!shape_ok(shape) || B > 128 || tree->max_nodes > MAX_TREE_NODES) return SOL_ERR_UNSUPPORTED;
+  for (int l = 0; l < n_layers; ++l)
+    if (!cache_size_ok(shape, &kvs[l])) return SOL_ERR_UNSUPPORTED;
+  if (B == 0) return SOL_OK;
+  launch_tree_commit(*shape, n_layers, kvs, *tree, B, path, path_len, new_lens, at<int>(ws, 0), (cudaStream_t)stream);
+  return finish();
+}
+
+sol_status_t sol_weighted_decode_attn(const sol_shape_t* shape, const void* q_bf16, const sol_kv_t* kv, int32_t B, float decay,
+                                      float* weights, void* out_bf16, void* ws, size_t ws_bytes, sol_stream_t stream) {
+  if (!shape || !q_bf16 || !kv_ok(kv) || !weights || !out_bf16 || !ws || B < 0 || !(decay >= 0.f && decay <= 1.f))
+    return SOL_ERR_INVALID_ARG;
+  if (!aligned16(q_bf16) || !aligned16(out_bf16) || !aligned16(kv->k_pool) || !aligned16(kv->v_pool) || !aligned16(weights) ||
+      !aligned16(ws))
+    return SOL_ERR_INVALID_ARG;
+  if (!shape_ok(shape) || B > 128 || !cache_size_ok(shape, kv)) return SOL_ERR_UNSUPPORTED;
+  if (B == 0) return SOL_OK;
+  const Layout L = make_layout(*shape, B, kv->max_pages_per_seq);
+  if (ws_bytes < L.total) return SOL_ERR_WORKSPACE_TOO_SMALL;
+  RowsArgs a;
+  memset(&a, 0, sizeof(a));
+  a.shape = *shape; a.kv = *kv; a.B = B; a.max_nodes = 1;
+  a.q = q_bf16; a.out = out_bf16;
+  a.part = at<float>(ws, L.attn.row_hist); a.part_bytes = L.attn.work_ctr - L.attn.row_hist;  // row_hist .. part lie side by side
+  a.weights = weights; a.decay = decay;
+  a.logits = at<float>(ws, L.attn.logits); a.lse = at<float>(ws, L.attn.q_rot);
+  a.status = at<int>(ws, L.status);
+  launch_rows_attention(a, (cudaStream_t)stream);
+  return finish();
+}
+
+sol_status_t sol_kv_evict(const sol_shape_t* shape, const sol_kv_t* kv, int32_t B, const int32_t* budgets, const float* weights,
+                          const int32_t* dst_table, float* dst_weights, int32_t* dst_lens, int32_t* kept_idx, void* ws,
+                          size_t ws_bytes, sol_stream_t stream) {
+  if (!shape || !kv_ok(kv) || !budgets || !weights || !dst_table || !dst_weights || !dst_lens || !ws || B < 0)
+    return SOL_ERR_INVALID_ARG;
+  if (!aligned16(kv->k_pool) || !aligned16(kv->v_pool) || !aligned16(ws) || dst_lens == kv->seq_lens) return SOL_ERR_INVALID_ARG;
+  if (!shape_ok(shape) || B > 128 || !cache_size_ok(shape, kv)) return SOL_ERR_UNSUPPORTED;
+  if (B == 0) return SOL_OK;
+  const Layout L = make_layout(*shape, B, kv->max_pages_per_seq);
+  if (ws_bytes < L.total) return SOL_ERR_WORKSPACE_TOO_SMALL;
+  EvictArgs a;
+  memset(&a, 0, sizeof(a));
+  a.shape = *shape; a.kv = *kv; a.B = B; a.budgets = budgets; a.weights = weights;
+  a.dst_table = dst_table; a.dst_weights = dst_weights; a.dst_lens = dst_lens;
+  a.kept_idx = kept_idx ? kept_idx : at<int32_t>(ws, L.attn.kept_idx);
+  a.status = at<int>(ws, L.status);
+  launch_evict(a, (cudaStream_t)stream);
   return finish();
 }
 

@@ -1,0 +1,135 @@
+// Work sharing of the dense attention kernels over the paged cache (trees of drafted tokens, decode steps that keep the
+// attention weights).
+//
+// A chain is what one softmax runs along: a (sequence, kv-head, block of query rows) over the sequence's cache pages.  The
+// pages of all chains, one chain after the other, form one line of tiles, and every CTA takes an equal run of it, whatever
+// the lengths are.  A run covers the end of one chain, some whole chains and the beginning of another: results of whole chains
+// go straight to the output, the first and the last piece go to one of the CTA's two slots of partial results, and a second
+// kernel merges the chains that were cut.  Every CTA of either kernel makes the line for itself from the lengths (at most 128).
+#pragma once
+#include "sol_common.cuh"
+#include "sol_internal.h"
+
+namespace sol {
+
+constexpr int CHAIN_MAX_BATCH = 128;
+
+// What the kernels know of a sequence: T tokens in the cache, the last n of them drafted.
+struct ChainSeq {
+  int T, n;
+};
+// n_nodes == nullptr: a decode step, one query token per sequence, which is the newest token (an empty sequence has it too: its
+// output is zero).
+__device__ __forceinline__ ChainSeq chain_seq(const sol_kv_t& kv, const int32_t* n_nodes, int max_nodes, int b, int* status) {
+  ChainSeq s;
+  const int len = kv.seq_lens[b], room = kv.max_pages_per_seq * PAGE;
+  s.T = min(max(len, 0), room);
+  s.n = 1;
+  if (n_nodes) {
+    const int n = n_nodes[b];
+    s.n = min(min(max(n, 0), max_nodes), s.T);
+    if (status && (s.n != n || s.T != len)) atomicOr(status + ST_ERR, ERR_BAD_ACTION);
+  }
+  return s;
+}
+
+// The line of tiles.  cum[b]: tiles of the sequences before b; seq: lengths.
+struct ChainPlan {
+  int cum[CHAIN_MAX_BATCH + 1];
+  ChainSeq seq[CHAIN_MAX_BATCH];
+  int wsum[4];
+};
+
+struct ChainShape {
+  sol_kv_t kv;
+  int B, Hkv, G, max_nodes;
+  const int32_t* n_nodes;  // nullptr: decode steps
+  int block_rows;          // query rows of a chain
+  int min_tiles;           // tiles of a CTA's run at least
+};
+
+__device__ __forceinline__ int chain_tiles(const ChainSeq& s) { return max(1, (s.T + PAGE - 1) / PAGE); }
+__device__ __forceinline__ int chain_blocks(const ChainShape& c, const ChainSeq& s) { return (s.n * c.G + c.block_rows - 1) / c.block_rows; }
+
+// By the whole CTA (128 threads at least); ends with a barrier.
+__device__ __forceinline__ void chain_plan(const ChainShape& c, ChainPlan& p, int* status) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  int tiles = 0;
+  if (tid < CHAIN_MAX_BATCH) {
+    ChainSeq s;
+    s.T = s.n = 0;
+    if (tid < c.B) {
+      s = chain_seq(c.kv, c.n_nodes, c.max_nodes, tid, status);
+      tiles = s.n > 0 ? chain_tiles(s) * chain_blocks(c, s) * c.Hkv : 0;
+    }
+    p.seq[tid] = s;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, tiles, o);
+      if (lane >= o) tiles += x;
+    }
+    if (lane == 31) p.wsum[warp] = tiles;
+  }
+  __syncthreads();
+  if (tid < CHAIN_MAX_BATCH) {
+    for (int w = 0; w < warp; ++w) tiles += p.wsum[w];
+    p.cum[tid + 1] = tiles;
+    if (tid == 0) p.cum[0] = 0;
+  }
+  __syncthreads();
+}
+
+// Tiles of a CTA's run, for `ctas` CTAs.
+__device__ __forceinline__ int chain_run(const ChainShape& c, const ChainPlan& p, int ctas) {
+  return max(c.min_tiles, (p.cum[c.B] + ctas - 1) / ctas);
+}
+
+// The sequence that holds tile u of the line.
+__device__ __forceinline__ int chain_find(const ChainShape& c, const ChainPlan& p, int u) {
+  int lo = 0, hi = c.B - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (p.cum[mid] <= u) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+// A run's next piece: tiles [tile0, tile1) of a chain.
+struct ChainPiece {
+  int b, kvh, block;
+  int tile0, tile1, tiles;  // tiles: of the whole chain
+  ChainSeq seq;
+  __device__ __forceinline__ bool whole() const { return tile0 == 0 && tile1 == tiles; }
+};
+__device__ __forceinline__ ChainPiece chain_piece(const ChainShape& c, const ChainPlan& p, int u, int end) {
+  ChainPiece r;
+  r.b = chain_find(c, p, u);
+  r.seq = p.seq[r.b];
+  r.tiles = chain_tiles(r.seq);
+  const int local = u - p.cum[r.b], chain = local / r.tiles, blocks = chain_blocks(c, r.seq);
+  r.tile0 = local - chain * r.tiles;
+  r.tile1 = min(r.tiles, r.tile0 + end - u);
+  r.kvh = chain / blocks;
+  r.block = chain - r.kvh * blocks;
+  return r;
+}
+
+// Where the pieces of a cut chain lie: CTAs first .. last, of which the first one's piece is in its slot 1 unless the chain
+// begins with its run; the others' are in slot 0.
+struct ChainCut {
+  int first, last, first_slot;
+  __device__ __forceinline__ bool cut() const { return last > first; }
+  __device__ __forceinline__ int slot(int i) const { return i == 0 ? first_slot : 2 * (first + i); }  // of piece i
+  __device__ __forceinline__ int pieces() const { return last - first + 1; }
+};
+__device__ __forceinline__ ChainCut chain_cut(const ChainShape& c, const ChainPlan& p, int run, int b, int chain) {
+  const int tiles = chain_tiles(p.seq[b]), u0 = p.cum[b] + chain * tiles;
+  ChainCut r;
+  r.first = u0 / run;
+  r.last = (u0 + tiles - 1) / run;
+  r.first_slot = 2 * r.first + (u0 % run ? 1 : 0);
+  return r;
+}
+
+}  // namespace sol

@@ -340,6 +340,53 @@ inline void attn_scratch_bind(AttnArgs& a, void* base, const AttnScratch& L, int
 }
 void launch_attention(const AttnArgs& a, cudaStream_t st);
 
+// ---- dense attention over the cache: trees of drafted tokens, decode steps with weights (sol_rows_attn.cu) ----
+struct RowsArgs {
+  sol_shape_t shape;
+  sol_kv_t kv;
+  int B, max_nodes;         // decode steps: max_nodes 1
+  const int32_t* n_nodes;   // [B]; nullptr: decode steps
+  const uint64_t* mask;     // [B][max_nodes]; nullptr: decode steps
+  const void* q;            // bf16 [B][max_nodes][Hq][hd]
+  void* out;                // same
+  float* part;              // scratch for the chains that are cut between CTAs
+  size_t part_bytes;
+  float* weights;           // optional, decode steps: [B][Hkv][max_pages * 64], updated: decay * old + this step's
+  float decay;
+  float* logits;            // scratch, with weights: [B][Hkv][G][max_pages * 64]
+  float* lse;               // scratch, with weights: [B][Hq]
+  int* status;
+};
+size_t rows_part_bytes(const sol_shape_t& sh);
+void launch_rows_attention(const RowsArgs& a, cudaStream_t st);
+// Tensor map of a pool's rows: boxes of 64 elements x box_rows rows, 128-byte swizzle.  False (and a recorded error) if it fails.
+bool encode_pool_map(struct CUtensorMap_st* map, const void* pool, const sol_shape_t& sh, int num_pages, int box_rows);
+
+// ---- bookkeeping of drafted trees (sol_tree.cu) ----------------------------
+constexpr int MAX_TREE_NODES = 64;
+constexpr int COMMIT_LAYERS = 64;  // layers per launch of tree_commit_kernel
+void launch_tree_build(int B, int max_nodes, const int32_t* n_nodes, const int32_t* parents, uint64_t* mask, int32_t* depth,
+                       cudaStream_t st);
+void launch_tree_accept(int B, int max_nodes, const int32_t* n_nodes, const int32_t* parents, const int32_t* draft,
+                        const int32_t* target, int32_t* path, int32_t* path_len, int32_t* next_token, cudaStream_t st);
+void launch_tree_commit(const sol_shape_t& sh, int n_layers, const sol_kv_t* kvs, const sol_tree_t& tree, int B,
+                        const int32_t* path, const int32_t* path_len, int32_t* new_lens, int* status, cudaStream_t st);
+
+// ---- eviction (sol_evict.cu) -------------------------------------------------
+struct EvictArgs {
+  sol_shape_t shape;
+  sol_kv_t kv;
+  int B;
+  const int32_t* budgets;      // [B]
+  const float* weights;        // [B][Hkv][max_pages * 64]
+  const int32_t* dst_table;    // [B][max_pages]
+  float* dst_weights;          // as weights
+  int32_t* dst_lens;           // [B]
+  int32_t* kept_idx;           // [B][Hkv][max_pages * 64]
+  int* status;
+};
+void launch_evict(const EvictArgs& a, cudaStream_t st);
+
 // ---- MLP channel selection (sol_mlp.cu) -------------------------------------
 struct ChannelSelectArgs {
   int B, d, ff;

@@ -1,0 +1,556 @@
+// Dense attention of few query rows over the paged cache: the decode step that keeps the attention weights
+// (sol_weighted_decode_attn) and small trees of drafted tokens (sol_tree_attn).
+//
+//   o_r = sum_t p_rt v_t,  p_rt = 2^(s_rt - m_r) / l_r,  s_rt = (q_r . k_t) log2(e) / sqrt(head_dim)  where row r sees token t
+//
+//   rows_attn_kernel   one CTA per SM takes its run of tiles (sol_chain.cuh; a tile is a 64-token page of one kv-head).  A
+//                      producer warp brings keys and values by TMA (128-byte swizzle) in steps of 16 KB, which the other
+//                      warps take in turn, each into its own ring of stages: 16 query rows are the M side of mma.sync
+//                      m16n8k16, online softmax in registers, weights as bf16 high and low parts.  At the end of a chain
+//                      the warps' results are merged through shared memory.
+//   rows_merge_kernel  merges the chains that were cut between CTAs.
+//   weight_kernel      the same for decode steps, and then the weights: w_t <- decay w_t + sum_g 2^(s_gt - lse_g) from the
+//                      logits that the first kernel left.
+#include <cuda.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "sol_chain.cuh"
+#include "sol_umma.cuh"
+
+namespace sol {
+
+constexpr int RA_ROWS = 16;   // query rows of a chain
+constexpr int RA_WARPS = 6;   // consumer warps
+constexpr int RA_DEPTH = 2;   // stages of a warp's ring
+constexpr int RA_THREADS = (RA_WARPS + 1) * 32;
+constexpr int RA_MIN_TILES = 4;
+
+struct RowsDev {
+  ChainShape c;
+  int Hq;
+  float scale_log2;      // log2(e) / sqrt(head_dim)
+  const uint64_t* mask;  // [B][max_nodes]; nullptr: a decode step
+  const uint16_t* q;     // [B][max_nodes][Hq][HD]
+  uint16_t* out;
+  float* part;           // [2 gridDim.x][part_rows][HD + 2]: sums, maximum (base 2), sum of the weights
+  int part_rows;         // query rows a chain has at most
+  float* logits;         // decode steps with weights: [B][Hkv][G][Tmax] base-2 logits, else nullptr
+  float* lse;            // ... [B][Hq] base-2 log of the weights' sum (infinite where no token counts), of chains that were not cut
+  int* status;
+};
+
+// Tokens of a step (16 KB of keys and values), bytes of its keys, floats that a lane hands over in a merge.
+template <int HD>
+struct RaSize {
+  static constexpr int TOK = HD == 64 ? 64 : 32;
+  static constexpr int STEPS = PAGE / TOK;     // of a tile
+  static constexpr int HALF = TOK * 128;       // a 64-wide half of the keys: [TOK tokens][128 B]
+  static constexpr int TILE = HALF * (HD / 64);
+  static constexpr int STAGES = RA_WARPS * RA_DEPTH;
+  static constexpr int REGS = HD / 8 * 4 + 4;  // sums, two maxima, two sums of weights
+  static constexpr int MERGE = 2 * REGS * 32 * 4;
+  static constexpr int SMEM = 1024 + STAGES * 2 * TILE + MERGE;
+};
+
+// Shared-memory address of 16-byte piece c of token r of a step.
+template <int HD>
+__device__ __forceinline__ uint32_t ra_piece(uint32_t base, int r, int c) {
+  return base + (uint32_t)((c >> 3) * RaSize<HD>::HALF + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+}
+__device__ __forceinline__ void ra_consumer_sync() { asm volatile("bar.sync 1, %0;" ::"n"(RA_WARPS * 32) : "memory"); }
+
+template <int HD>
+__global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_constant__ CUtensorMap kmap,
+                                                                  const __grid_constant__ CUtensorMap vmap, const RowsDev p) {
+  using Z = RaSize<HD>;
+  constexpr int KS = HD / 16, ND = HD / 8, NT = Z::TOK / 8;
+  extern __shared__ unsigned char ra_smem[];
+  __shared__ ChainPlan plan;
+  __shared__ uint64_t full[Z::STAGES], empty[Z::STAGES];
+  __shared__ int page_ok[Z::STAGES];
+  unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(ra_smem) + 1023) & ~(uintptr_t)1023);
+  float* merge = reinterpret_cast<float*>(ring + Z::STAGES * 2 * Z::TILE);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int s = 0; s < Z::STAGES; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    fence_mbar_init();
+    tma_prefetch_map(&kmap);
+    tma_prefetch_map(&vmap);
+  }
+  pdl_wait();
+  pdl_trigger();
+  chain_plan(p.c, plan, blockIdx.x == 0 ? p.status : nullptr);
+  const int run = chain_run(p.c, plan, gridDim.x);
+  const int u0 = (int)min((long long)blockIdx.x * run, (long long)plan.cum[p.c.B]), u1 = min(plan.cum[p.c.B], u0 + run);
+
+  if (warp == RA_WARPS) {  // ---- the producer ----
+    int it = 0;
+    for (int u = u0; u < u1;) {
+      const ChainPiece c = chain_piece(p.c, plan, u, u1);
+      const int32_t* table = p.c.kv.page_table + (size_t)c.b * p.c.kv.max_pages_per_seq;
+      for (int g0 = c.tile0; g0 < c.tile1; g0 += 32) {
+        int mine = 0;
+        if (g0 + lane < c.tile1 && c.seq.T > 0) mine = table[g0 + lane];
+        const int cnt = min(32, c.tile1 - g0);
+        for (int x = 0; x < cnt * Z::STEPS; ++x, ++it) {
+          int page = __shfl_sync(0xffffffffu, mine, x / Z::STEPS);
+          // step `it` goes to warp it % RA_WARPS, whose use number `use` of its ring it is
+          const int use = it / RA_WARPS, st = it % RA_WARPS * RA_DEPTH + use % RA_DEPTH;
+          if (use >= RA_DEPTH && !mbar_wait(&empty[st], (use / RA_DEPTH - 1) & 1, p.status)) return;  // the consumers give up too
+          if (lane == 0) {
+            const bool ok = page >= 0 && page < p.c.kv.num_pages;
+            if (!ok) {
+              atomicOr(p.status + ST_ERR, ERR_BAD_PAGE);
+              page = 0;  // some memory of the pool; none of its tokens is seen
+            }
+            page_ok[st] = ok;
+            unsigned char* dst = ring + (size_t)st * 2 * Z::TILE;
+            mbar_expect_tx(&full[st], 2 * Z::TILE);
+            const int row = (page * p.c.Hkv + c.kvh) * PAGE + x % Z::STEPS * Z::TOK;
+#pragma unroll
+            for (int h = 0; h < HD / 64; ++h) {
+              tma_load_2d(dst + h * Z::HALF, &kmap, h * 64, row, &full[st]);
+              tma_load_2d(dst + Z::TILE + h * Z::HALF, &vmap, h * 64, row, &full[st]);
+            }
+          }
+          __syncwarp();
+        }
+      }
+      u += c.tile1 - c.tile0;
+    }
+    return;
+  }
+
+  // ---- the consumers ----
+  const int g = lane >> 2, t = lane & 3, G = p.c.G;
+  int it = 0;
+  bool alive = true;
+  for (int u = u0; u < u1;) {
+    const ChainPiece c = chain_piece(p.c, plan, u, u1);
+    const int C = c.seq.T - c.seq.n, T = c.seq.T, rows = c.seq.n * G;
+    // this lane's rows: r0 = block * 16 + g and r0 + 8
+    uint32_t q[KS][4];
+    uint64_t seen[2];
+    const int r0 = c.block * RA_ROWS + g;
+    size_t base[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = r0 + 8 * h, node = r / G;
+      base[h] = (((size_t)c.b * p.c.max_nodes + node) * p.Hq + c.kvh * G + (r - node * G)) * HD;
+      seen[h] = r < rows ? (p.mask ? p.mask[(size_t)c.b * p.c.max_nodes + node] : ~0ull) : 0ull;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(p.q + base[h] + k * 16 + 2 * t);
+        q[k][h] = r < rows ? src[0] : 0u;
+        q[k][2 + h] = r < rows ? src[4] : 0u;
+      }
+    }
+    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+    float o[ND][4];
+#pragma unroll
+    for (int j = 0; j < ND; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+
+    const int len = (c.tile1 - c.tile0) * Z::STEPS;
+    for (int x = (warp - it % RA_WARPS + RA_WARPS) % RA_WARPS; x < len; x += RA_WARPS) {
+      const int use = (it + x) / RA_WARPS, st = warp * RA_DEPTH + use % RA_DEPTH;
+      const int tok0 = c.tile0 * PAGE + x * Z::TOK;  // first token of the step
+      alive = alive && mbar_wait(&full[st], (use / RA_DEPTH) & 1, p.status);
+      if (!alive) break;
+      const uint32_t kb = smem_u32(ring + (size_t)st * 2 * Z::TILE), vb = kb + Z::TILE;
+      const bool ok = page_ok[st] != 0;
+      float sc[NT][4];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) sc[j][0] = sc[j][1] = sc[j][2] = sc[j][3] = 0.f;
+#pragma unroll
+      for (int k2 = 0; k2 < KS / 2; ++k2) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          uint32_t bb[4];
+          ldsm_x4(bb, ra_piece<HD>(kb, j * 8 + (lane & 7), k2 * 4 + (lane >> 3)));
+          mma_bf16(sc[j], q[2 * k2][0], q[2 * k2][1], q[2 * k2][2], q[2 * k2][3], bb[0], bb[1]);
+          mma_bf16(sc[j], q[2 * k2 + 1][0], q[2 * k2 + 1][1], q[2 * k2 + 1][2], q[2 * k2 + 1][3], bb[2], bb[3]);
+        }
+      }
+      // ---- which tokens are seen; a tile inside the context is seen whole by every row ----
+      uint64_t bad = 0;  // drafted tokens of the step with values that are not finite
+      if (ok && tok0 + Z::TOK <= C) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[j][e] *= p.scale_log2;
+      } else {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int tok = tok0 + j * 8 + 2 * t + (e & 1);
+            const bool s = ok && (tok < C || (tok < T && ((seen[e >> 1] >> (tok - C)) & 1)));
+            sc[j][e] = s ? sc[j][e] * p.scale_log2 : -INFINITY;
+          }
+        // A weight of zero must not meet a value that is not finite.  Rows of the page behind the sequence are cleared, and so
+        // are drafted tokens' rows with such values, which are added below for the query rows that see them.
+#pragma unroll
+        for (int w = 0; w < Z::TOK / 32; ++w) {
+          const int r = lane + 32 * w, tok = tok0 + r;
+          bool drop = tok >= T || !ok;
+          if (!drop && tok >= C) {
+            for (int cc = 0; cc < HD / 8; ++cc) {
+              const uint4 v = lds128(ra_piece<HD>(vb, r, cc));
+              const uint32_t x4[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                drop = drop || (x4[e] & 0x7f80u) == 0x7f80u || (x4[e] & 0x7f800000u) == 0x7f800000u;
+            }
+          }
+          if (drop)
+            for (int cc = 0; cc < HD / 8; ++cc)
+              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ra_piece<HD>(vb, r, cc)), "r"(0u) : "memory");
+          const uint32_t votes = __ballot_sync(0xffffffffu, drop && ok && tok >= C && tok < T);
+          bad |= (uint64_t)votes << (32 * w);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // ahead of the TMA write that takes the stage next
+        __syncwarp();
+      }
+      if (p.logits) {  // decode steps: the G heads are rows 0 .. G - 1
+        if (g < G) {
+          const size_t stride = (size_t)p.c.kv.max_pages_per_seq * PAGE;
+          float* dst = p.logits + (((size_t)c.b * p.c.Hkv + c.kvh) * G + g) * stride + tok0 + 2 * t;
+#pragma unroll
+          for (int j = 0; j < NT; ++j) *reinterpret_cast<float2*>(dst + j * 8) = make_float2(sc[j][0], sc[j][1]);
+        }
+      }
+      float x0 = -INFINITY, x1 = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        x0 = fmaxf(x0, fmaxf(sc[j][0], sc[j][1]));
+        x1 = fmaxf(x1, fmaxf(sc[j][2], sc[j][3]));
+      }
+#pragma unroll
+      for (int off = 1; off <= 2; off <<= 1) {
+        x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, off));
+        x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, off));
+      }
+      const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
+      const float b0 = n0 == -INFINITY ? 0.f : n0, b1 = n1 == -INFINITY ? 0.f : n1;  // a row that has seen nothing yet
+      const float f0 = exp2f(m0 - b0), f1 = exp2f(m1 - b1);
+      m0 = n0;
+      m1 = n1;
+      l0 *= f0;
+      l1 *= f1;
+#pragma unroll
+      for (int j = 0; j < ND; ++j) {
+        o[j][0] *= f0;
+        o[j][1] *= f0;
+        o[j][2] *= f1;
+        o[j][3] *= f1;
+      }
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        sc[j][0] = exp2f(sc[j][0] - b0);
+        sc[j][1] = exp2f(sc[j][1] - b0);
+        sc[j][2] = exp2f(sc[j][2] - b1);
+        sc[j][3] = exp2f(sc[j][3] - b1);
+        l0 += sc[j][0] + sc[j][1];
+        l1 += sc[j][2] + sc[j][3];
+      }
+#pragma unroll
+      for (int kk = 0; kk < NT / 2; ++kk) {
+        uint32_t ph[4], pl[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {  // n-tile 2 kk + (y >> 1), row half y & 1
+          const float v0 = sc[2 * kk + (y >> 1)][(y & 1) * 2], v1 = sc[2 * kk + (y >> 1)][(y & 1) * 2 + 1];
+          const uint16_t h0 = f2bf(v0), h1 = f2bf(v1);
+          ph[y] = (uint32_t)h0 | ((uint32_t)h1 << 16);
+          pl[y] = pack_bf16(v0 - bf2f(h0), v1 - bf2f(h1));
+        }
+#pragma unroll
+        for (int j2 = 0; j2 < ND / 2; ++j2) {
+          uint32_t bb[4];
+          ldsm_x4_trans(bb, ra_piece<HD>(vb, kk * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), j2 * 2 + (lane >> 4)));
+          mma_bf16(o[2 * j2], ph[0], ph[1], ph[2], ph[3], bb[0], bb[1]);
+          mma_bf16(o[2 * j2], pl[0], pl[1], pl[2], pl[3], bb[0], bb[1]);
+          mma_bf16(o[2 * j2 + 1], ph[0], ph[1], ph[2], ph[3], bb[2], bb[3]);
+          mma_bf16(o[2 * j2 + 1], pl[0], pl[1], pl[2], pl[3], bb[2], bb[3]);
+        }
+      }
+      if (bad) {  // p v in float32 for the rows that see such a token, from the cache
+        const int page = p.c.kv.page_table[(size_t)c.b * p.c.kv.max_pages_per_seq + tok0 / PAGE];
+        const uint16_t* v =
+            static_cast<const uint16_t*>(p.c.kv.v_pool) + (((size_t)page * p.c.Hkv + c.kvh) * PAGE + tok0 % PAGE) * HD;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {  // tokens 8 j + e: weights in lane e >> 1 of each quad
+            const float p0 = __shfl_sync(0xffffffffu, sc[j][e & 1], g * 4 + (e >> 1));
+            const float p1 = __shfl_sync(0xffffffffu, sc[j][2 + (e & 1)], g * 4 + (e >> 1));
+            if (!((bad >> (8 * j + e)) & 1)) continue;
+            const int node = tok0 + 8 * j + e - C;
+            const bool s0 = (seen[0] >> node) & 1, s1 = (seen[1] >> node) & 1;
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+              const uint32_t w = *reinterpret_cast<const uint32_t*>(v + (8 * j + e) * HD + d * 8 + 2 * t);
+              if (s0) {
+                o[d][0] += p0 * bf16_lo(w);
+                o[d][1] += p0 * bf16_hi(w);
+              }
+              if (s1) {
+                o[d][2] += p1 * bf16_lo(w);
+                o[d][3] += p1 * bf16_hi(w);
+              }
+            }
+          }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&empty[st]);
+    }
+    it += len;
+
+    // ---- merge the warps, 4 and 5 into 0 and 1, then 2 and 3, then 1; a lane holds the same elements in every warp ----
+#pragma unroll 1
+    for (int half = 4; half; half >>= 1) {
+      float* slot = merge + (size_t)(warp & 1 & (half - 1)) * Z::REGS * 32 + lane;
+      const bool gives = warp >= half && warp < min(2 * half, RA_WARPS), takes = warp + half < min(2 * half, RA_WARPS);
+      if (gives) {
+#pragma unroll
+        for (int j = 0; j < ND; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) slot[(j * 4 + e) * 32] = o[j][e];
+        slot[(ND * 4) * 32] = m0;
+        slot[(ND * 4 + 1) * 32] = m1;
+        slot[(ND * 4 + 2) * 32] = l0;
+        slot[(ND * 4 + 3) * 32] = l1;
+      }
+      ra_consumer_sync();
+      if (takes) {
+        const float y0 = slot[(ND * 4) * 32], y1 = slot[(ND * 4 + 1) * 32];
+        const float n0 = fmaxf(m0, y0), n1 = fmaxf(m1, y1);
+        const float b0 = n0 == -INFINITY ? 0.f : n0, b1 = n1 == -INFINITY ? 0.f : n1;
+        const float f0 = exp2f(m0 - b0), f1 = exp2f(m1 - b1), h0 = exp2f(y0 - b0), h1 = exp2f(y1 - b1);
+        m0 = n0;
+        m1 = n1;
+        l0 = l0 * f0 + slot[(ND * 4 + 2) * 32] * h0;
+        l1 = l1 * f1 + slot[(ND * 4 + 3) * 32] * h1;
+#pragma unroll
+        for (int j = 0; j < ND; ++j) {
+          o[j][0] = o[j][0] * f0 + slot[(j * 4) * 32] * h0;
+          o[j][1] = o[j][1] * f0 + slot[(j * 4 + 1) * 32] * h0;
+          o[j][2] = o[j][2] * f1 + slot[(j * 4 + 2) * 32] * h1;
+          o[j][3] = o[j][3] * f1 + slot[(j * 4 + 3) * 32] * h1;
+        }
+      }
+      ra_consumer_sync();
+    }
+    if (warp == 0) {
+#pragma unroll
+      for (int off = 1; off <= 2; off <<= 1) {
+        l0 += __shfl_xor_sync(0xffffffffu, l0, off);
+        l1 += __shfl_xor_sync(0xffffffffu, l1, off);
+      }
+      const bool whole = c.whole();
+      float* part = p.part + (size_t)(2 * blockIdx.x + (u > u0)) * p.part_rows * (HD + 2);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int r = r0 + 8 * h;
+        if (r >= rows) continue;
+        const float l = h ? l1 : l0, m = h ? m1 : m0;
+        if (whole) {
+          const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+          for (int j = 0; j < ND; ++j)
+            *reinterpret_cast<uint32_t*>(p.out + base[h] + j * 8 + 2 * t) = pack_bf16(o[j][2 * h] * inv, o[j][2 * h + 1] * inv);
+          if (p.lse && t == 0) p.lse[(size_t)c.b * p.Hq + c.kvh * G + r] = l == 0.f ? INFINITY : m + log2f(l);
+        } else {
+          float* dst = part + (size_t)(g + 8 * h) * (HD + 2);
+#pragma unroll
+          for (int j = 0; j < ND; ++j)
+            *reinterpret_cast<float2*>(dst + j * 8 + 2 * t) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
+          if (t == 0) *reinterpret_cast<float2*>(dst + HD) = make_float2(m, l);
+        }
+      }
+    }
+    u += c.tile1 - c.tile0;
+  }
+}
+
+// ---- merge of the chains that were cut -----------------------------------------------------------
+constexpr int RM_THREADS = 256;
+
+// Factors of a chain's pieces: row r of piece i counts 2^(m_i - M) / sum_i l_i 2^(m_i - M).  fac: [pieces][rows].  By the whole
+// CTA; a warp takes a row at a time.  lse (optional): base-2 log of the row's sum.
+__device__ __forceinline__ void chain_factors(const ChainCut& cut, const float* part, int part_rows, int stride, int rows, float* fac,
+                                              float* lse) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, np = cut.pieces();
+  for (int r = warp; r < rows; r += blockDim.x >> 5) {
+    auto ml = [&](int i) {
+      return *reinterpret_cast<const float2*>(part + ((size_t)cut.slot(i) * part_rows + r) * stride + stride - 2);
+    };
+    float m = -INFINITY;
+    for (int i = lane; i < np; i += 32) m = fmaxf(m, ml(i).x);
+    m = warp_max(m);
+    const float base = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    for (int i = lane; i < np; i += 32) {
+      const float2 v = ml(i);
+      l += v.y * exp2f(v.x - base);
+    }
+    l = warp_sum(l);
+    const float inv = l == 0.f ? 0.f : 1.0f / l;  // a row that sees nothing
+    for (int i = lane; i < np; i += 32) fac[(size_t)i * rows + r] = exp2f(ml(i).x - base) * inv;
+    if (lse && lane == 0) lse[r] = l == 0.f ? INFINITY : base + log2f(l);
+  }
+}
+
+template <int HD>
+__device__ __forceinline__ void chain_merge(const RowsDev& p, const ChainCut& cut, const float* fac, int rows, int b, int kvh, int block) {
+  const int np = cut.pieces();
+  for (int e = (int)threadIdx.x * 2; e < rows * HD; e += RM_THREADS * 2) {
+    const int r = e / HD, d = e - r * HD;
+    float2 a = make_float2(0.f, 0.f);
+#pragma unroll 8
+    for (int i = 0; i < np; ++i) {
+      const float2 v = *reinterpret_cast<const float2*>(p.part + ((size_t)cut.slot(i) * p.part_rows + r) * (HD + 2) + d);
+      const float f = fac[(size_t)i * rows + r];
+      a.x += f * v.x;
+      a.y += f * v.y;
+    }
+    const int row = block * RA_ROWS + r, node = row / p.c.G;
+    *reinterpret_cast<uint32_t*>(p.out + (((size_t)b * p.c.max_nodes + node) * p.Hq + kvh * p.c.G + (row - node * p.c.G)) * HD + d) =
+        pack_bf16(a.x, a.y);
+  }
+}
+
+template <int HD>
+__global__ void __launch_bounds__(RM_THREADS) rows_merge_kernel(const RowsDev p, int ctas) {
+  extern __shared__ float rm_fac[];  // [pieces of a chain][RA_ROWS]
+  __shared__ ChainPlan plan;
+  pdl_trigger();
+  chain_plan(p.c, plan, nullptr);
+  const int run = chain_run(p.c, plan, ctas);
+  pdl_wait();
+  const int kvh = blockIdx.x;
+  for (int b = blockIdx.y; b < p.c.B; b += gridDim.y) {
+    const ChainSeq s = plan.seq[b];
+    const int blocks = s.n > 0 ? chain_blocks(p.c, s) : 0;
+    for (int block = blockIdx.z; block < blocks; block += gridDim.z) {
+      const ChainCut cut = chain_cut(p.c, plan, run, b, kvh * blocks + block);
+      if (!cut.cut()) continue;
+      const int rows = min(RA_ROWS, s.n * p.c.G - block * RA_ROWS);
+      __syncthreads();
+      chain_factors(cut, p.part, p.part_rows, HD + 2, rows, rm_fac, nullptr);
+      __syncthreads();
+      chain_merge<HD>(p, cut, rm_fac, rows, b, kvh, block);
+    }
+  }
+}
+
+// ---- the weights of a decode step ----------------------------------------------------------------
+constexpr int WK_TOKENS = RM_THREADS * 4;  // tokens of a unit
+
+template <int HD>
+__global__ void __launch_bounds__(RM_THREADS) weight_kernel(const RowsDev p, int ctas, float decay, float* __restrict__ weights) {
+  extern __shared__ float wk_fac[];
+  __shared__ ChainPlan plan;
+  __shared__ float lse[8];
+  __shared__ int units[CHAIN_MAX_BATCH + 1];
+  const int tid = threadIdx.x;
+  pdl_trigger();
+  chain_plan(p.c, plan, nullptr);
+  const int run = chain_run(p.c, plan, ctas), G = p.c.G;
+  if (tid == 0) {
+    int n = 0;
+    for (int b = 0; b < p.c.B; ++b) {
+      units[b] = n;
+      n += max(1, (plan.seq[b].T + WK_TOKENS - 1) / WK_TOKENS) * p.c.Hkv;
+    }
+    units[p.c.B] = n;
+  }
+  __syncthreads();
+  pdl_wait();
+  const size_t stride = (size_t)p.c.kv.max_pages_per_seq * PAGE;
+  for (int u = blockIdx.x; u < units[p.c.B]; u += gridDim.x) {
+    int lo = 0, hi = p.c.B - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (units[mid] <= u) lo = mid;
+      else hi = mid - 1;
+    }
+    const int b = lo, T = plan.seq[b].T, per = max(1, (T + WK_TOKENS - 1) / WK_TOKENS);
+    const int kvh = (u - units[b]) / per, chunk = (u - units[b]) - kvh * per;
+    const ChainCut cut = chain_cut(p.c, plan, run, b, kvh);
+    __syncthreads();
+    if (cut.cut()) chain_factors(cut, p.part, p.part_rows, HD + 2, G, wk_fac, lse);
+    else if (tid < G) lse[tid] = p.lse[(size_t)b * p.Hq + kvh * G + tid];
+    __syncthreads();
+    if (chunk == 0 && cut.cut()) chain_merge<HD>(p, cut, wk_fac, G, b, kvh, 0);
+    const int tok = chunk * WK_TOKENS + tid * 4;
+    if (tok >= T) continue;
+    const size_t bk = (size_t)b * p.c.Hkv + kvh;
+    float w[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int g = 0; g < G; ++g) {
+      const float4 s = *reinterpret_cast<const float4*>(p.logits + (bk * G + g) * stride + tok);
+      w[0] += exp2f(s.x - lse[g]);
+      w[1] += exp2f(s.y - lse[g]);
+      w[2] += exp2f(s.z - lse[g]);
+      w[3] += exp2f(s.w - lse[g]);
+    }
+    float* dst = weights + bk * stride + tok;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (tok + i < T) dst[i] = tok + i == T - 1 ? w[i] : decay * dst[i] + w[i];
+  }
+}
+
+// ---- host ----------------------------------------------------------------------------------------
+size_t rows_part_bytes(const sol_shape_t& sh) { return (size_t)2 * sm_count() * RA_ROWS * (sh.head_dim + 2) * 4; }
+
+template <int HD>
+static void launch_rows(const RowsDev& d, const CUtensorMap& kmap, const CUtensorMap& vmap, const RowsArgs& a, cudaStream_t st) {
+  // fewer CTAs where the caller's space for partial results is short
+  const int ctas = (int)std::min<size_t>(sm_count(), a.part_bytes / ((size_t)2 * d.part_rows * (HD + 2) * 4));
+  ensure_dynamic_smem(reinterpret_cast<const void*>(&rows_attn_kernel<HD>), RaSize<HD>::SMEM);
+  SOL_LAUNCH("rows_attn", rows_attn_kernel<HD>, dim3(ctas), dim3(RA_THREADS), RaSize<HD>::SMEM, st, kmap, vmap, d);
+  const int fac = ctas * RA_ROWS * 4;
+  if (a.weights) {
+    SOL_LAUNCH("attn_weights", weight_kernel<HD>, dim3(4 * ctas), dim3(RM_THREADS), fac, st, d, ctas, a.decay, a.weights);
+  } else {
+    const int blocks = (a.max_nodes * d.c.G + RA_ROWS - 1) / RA_ROWS;
+    SOL_LAUNCH("rows_merge", rows_merge_kernel<HD>, dim3(d.c.Hkv, d.c.B, blocks), dim3(RM_THREADS), fac, st, d, ctas);
+  }
+}
+
+void launch_rows_attention(const RowsArgs& a, cudaStream_t st) {
+  const sol_shape_t& sh = a.shape;
+  CUtensorMap kmap, vmap;
+  const int box = sh.head_dim == 64 ? RaSize<64>::TOK : RaSize<128>::TOK;
+  if (!encode_pool_map(&kmap, a.kv.k_pool, sh, a.kv.num_pages, box) ||
+      !encode_pool_map(&vmap, a.kv.v_pool, sh, a.kv.num_pages, box)) return;
+  RowsDev d;
+  memset(&d, 0, sizeof(d));
+  d.c.kv = a.kv;
+  d.c.B = a.B;
+  d.c.Hkv = sh.n_kv_heads;
+  d.c.G = sh.n_q_heads / sh.n_kv_heads;
+  d.c.max_nodes = a.max_nodes;
+  d.c.n_nodes = a.n_nodes;
+  d.c.block_rows = RA_ROWS;
+  d.c.min_tiles = RA_MIN_TILES;
+  d.Hq = sh.n_q_heads;
+  d.scale_log2 = 1.4426950408889634f / sqrtf((float)sh.head_dim);
+  d.mask = a.mask;
+  d.q = static_cast<const uint16_t*>(a.q);
+  d.out = static_cast<uint16_t*>(a.out);
+  d.part = a.part;
+  d.part_rows = a.weights ? d.c.G : RA_ROWS;
+  d.logits = a.weights ? a.logits : nullptr;
+  d.lse = a.weights ? a.lse : nullptr;
+  d.status = a.status;
+  if (sh.head_dim == 64) launch_rows<64>(d, kmap, vmap, a, st);
+  else launch_rows<128>(d, kmap, vmap, a, st);
+}
+
+}  // namespace sol
