@@ -794,11 +794,14 @@ static bool cache_size_ok(const sol_shape_t* s, const sol_kv_t* kv) {
 }
 static bool tree_ok(const sol_tree_t* t) { return t && t->n_nodes && t->mask && t->max_nodes >= 1; }
 
+// Which kernel takes a tree: a block of 16 query rows goes through mma.sync, more rows through tcgen05.
+static bool tree_by_rows(const sol_shape_t* s, int max_nodes) { return max_nodes * (s->n_q_heads / s->n_kv_heads) <= 16; }
+
 size_t sol_tree_workspace_bytes(const sol_shape_t* shape, int32_t max_batch, int32_t max_pages_per_seq, int32_t max_nodes) {
   if (!shape_ok(shape) || max_batch < 1 || max_batch > 128 || max_pages_per_seq < 1 || max_pages_per_seq > MAX_PAGES_PER_SEQ ||
       max_nodes < 1 || max_nodes > MAX_TREE_NODES || shape->n_kv_heads > 256)
     return 0;
-  return 256 + rows_part_bytes(*shape);
+  return 256 + (tree_by_rows(shape, max_nodes) ? rows_part_bytes(*shape) : tree_part_bytes(*shape, max_nodes));
 }
 
 sol_status_t sol_tree_build(int32_t B, int32_t max_nodes, const int32_t* n_nodes, const int32_t* parents, uint64_t* mask,
@@ -823,9 +826,10 @@ sol_status_t sol_tree_attn(const sol_shape_t* shape, const void* q_bf16, const s
   a.shape = *shape; a.kv = *kv; a.B = B;
   a.max_nodes = tree->max_nodes; a.n_nodes = tree->n_nodes; a.mask = tree->mask;
   a.q = q_bf16; a.out = out_bf16;
-  a.part = at<float>(ws, 256); a.part_bytes = rows_part_bytes(*shape);
+  a.part = at<float>(ws, 256); a.part_bytes = ws_bytes - 256;
   a.status = at<int>(ws, 0);
-  launch_rows_attention(a, (cudaStream_t)stream);
+  if (tree_by_rows(shape, tree->max_nodes)) launch_rows_attention(a, (cudaStream_t)stream);
+  else launch_tree_attention(a, (cudaStream_t)stream);
   return finish();
 }
 

@@ -1,9 +1,9 @@
 // Work sharing of the dense attention kernels over the paged cache (trees of drafted tokens, decode steps that keep the
 // attention weights).
 //
-// A chain is what one softmax runs along: a (sequence, kv-head, block of query rows) over the sequence's cache pages.  The
-// pages of all chains, one chain after the other, form one line of tiles, and every CTA takes an equal run of it, whatever
-// the lengths are.  A run covers the end of one chain, some whole chains and the beginning of another: results of whole chains
+// A chain is what one softmax runs along: a (sequence, kv-head, block of query rows) over the sequence's tokens, a tile of one
+// or two cache pages at a time.  The tiles of all chains, one chain after the other, form one line, and every CTA takes an
+// equal run of it, whatever the lengths are.  A run covers the end of one chain, some whole chains and the beginning of another: results of whole chains
 // go straight to the output, the first and the last piece go to one of the CTA's two slots of partial results, and a second
 // kernel merges the chains that were cut.  Every CTA of either kernel makes the line for itself from the lengths (at most 128).
 #pragma once
@@ -45,10 +45,25 @@ struct ChainShape {
   int B, Hkv, G, max_nodes;
   const int32_t* n_nodes;  // nullptr: decode steps
   int block_rows;          // query rows of a chain
+  int tile;                // tokens of a tile: PAGE or 2 PAGE
   int min_tiles;           // tiles of a CTA's run at least
 };
 
-__device__ __forceinline__ int chain_tiles(const ChainSeq& s) { return max(1, (s.T + PAGE - 1) / PAGE); }
+inline ChainShape chain_shape(const RowsArgs& a, int block_rows, int tile, int min_tiles) {
+  ChainShape c;
+  c.kv = a.kv;
+  c.B = a.B;
+  c.Hkv = a.shape.n_kv_heads;
+  c.G = a.shape.n_q_heads / a.shape.n_kv_heads;
+  c.max_nodes = a.max_nodes;
+  c.n_nodes = a.n_nodes;
+  c.block_rows = block_rows;
+  c.tile = tile;
+  c.min_tiles = min_tiles;
+  return c;
+}
+
+__device__ __forceinline__ int chain_tiles(const ChainShape& c, const ChainSeq& s) { return max(1, (s.T + c.tile - 1) / c.tile); }
 __device__ __forceinline__ int chain_blocks(const ChainShape& c, const ChainSeq& s) { return (s.n * c.G + c.block_rows - 1) / c.block_rows; }
 
 // By the whole CTA (128 threads at least); ends with a barrier.
@@ -60,7 +75,7 @@ __device__ __forceinline__ void chain_plan(const ChainShape& c, ChainPlan& p, in
     s.T = s.n = 0;
     if (tid < c.B) {
       s = chain_seq(c.kv, c.n_nodes, c.max_nodes, tid, status);
-      tiles = s.n > 0 ? chain_tiles(s) * chain_blocks(c, s) * c.Hkv : 0;
+      tiles = s.n > 0 ? chain_tiles(c, s) * chain_blocks(c, s) * c.Hkv : 0;
     }
     p.seq[tid] = s;
 #pragma unroll
@@ -106,7 +121,7 @@ __device__ __forceinline__ ChainPiece chain_piece(const ChainShape& c, const Cha
   ChainPiece r;
   r.b = chain_find(c, p, u);
   r.seq = p.seq[r.b];
-  r.tiles = chain_tiles(r.seq);
+  r.tiles = chain_tiles(c, r.seq);
   const int local = u - p.cum[r.b], chain = local / r.tiles, blocks = chain_blocks(c, r.seq);
   r.tile0 = local - chain * r.tiles;
   r.tile1 = min(r.tiles, r.tile0 + end - u);
@@ -124,12 +139,76 @@ struct ChainCut {
   __device__ __forceinline__ int pieces() const { return last - first + 1; }
 };
 __device__ __forceinline__ ChainCut chain_cut(const ChainShape& c, const ChainPlan& p, int run, int b, int chain) {
-  const int tiles = chain_tiles(p.seq[b]), u0 = p.cum[b] + chain * tiles;
+  const int tiles = chain_tiles(c, p.seq[b]), u0 = p.cum[b] + chain * tiles;
   ChainCut r;
   r.first = u0 / run;
   r.last = (u0 + tiles - 1) / run;
   r.first_slot = 2 * r.first + (u0 % run ? 1 : 0);
   return r;
 }
+
+// ---- partial results of cut chains ----
+// Per slot and row of a chain: HD weighted sums, and (maximum in the base-2 domain, sum of the weights).
+struct ChainParts {
+  float* sums;  // [slots][rows][HD]
+  float2* ml;   // [slots][rows]
+  int rows;
+};
+inline size_t chain_part_bytes(int ctas, int rows, int hd) { return (size_t)2 * ctas * rows * (hd * 4 + 8); }
+inline ChainParts chain_parts(void* base, int ctas, int rows, int hd) {
+  ChainParts p;
+  p.sums = static_cast<float*>(base);
+  p.ml = reinterpret_cast<float2*>(p.sums + (size_t)2 * ctas * rows * hd);
+  p.rows = rows;
+  return p;
+}
+
+// A row's merged maximum and 1 / (sum of the weights) (0 for a row that sees nothing), by the 16 lanes of half a warp.
+__device__ __forceinline__ float2 chain_merged_ml(const ChainParts& p, const ChainCut& cut, int row) {
+  const int sub = threadIdx.x & 15, np = cut.pieces();
+  float m = -INFINITY;
+  for (int i = sub; i < np; i += 16) m = fmaxf(m, p.ml[(size_t)cut.slot(i) * p.rows + row].x);
+#pragma unroll
+  for (int o = 8; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const float base = m == -INFINITY ? 0.f : m;
+  float l = 0.f;
+  for (int i = sub; i < np; i += 16) {
+    const float2 v = p.ml[(size_t)cut.slot(i) * p.rows + row];
+    l += v.y * exp2f(v.x - base);
+  }
+#pragma unroll
+  for (int o = 8; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  return make_float2(base, l);
+}
+
+// The merged row, HD / 16 of its columns per lane, as bf16 to dst (the row's first element).
+template <int HD>
+__device__ __forceinline__ void chain_merged_row(const ChainParts& p, const ChainCut& cut, int row, float2 ml, uint16_t* dst) {
+  constexpr int V = HD / 64;  // float4 per lane
+  const int sub = threadIdx.x & 15, np = cut.pieces();
+  const float inv = ml.y == 0.f ? 0.f : 1.0f / ml.y;
+  float4 a[V];
+#pragma unroll
+  for (int x = 0; x < V; ++x) a[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int i = 0; i < np; ++i) {
+    const size_t at = (size_t)cut.slot(i) * p.rows + row;
+    const float f = exp2f(p.ml[at].x - ml.x) * inv;
+#pragma unroll
+    for (int x = 0; x < V; ++x) {
+      const float4 v = *reinterpret_cast<const float4*>(p.sums + at * HD + x * 64 + sub * 4);
+      a[x].x += f * v.x;
+      a[x].y += f * v.y;
+      a[x].z += f * v.z;
+      a[x].w += f * v.w;
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < V; ++x)
+    *reinterpret_cast<uint2*>(dst + x * 64 + sub * 4) = make_uint2(pack_bf16(a[x].x, a[x].y), pack_bf16(a[x].z, a[x].w));
+}
+
+// Merges the cut chains of an attention kernel of `ctas` CTAs (sol_rows_attn.cu).
+void launch_chain_merge(const ChainShape& c, const ChainParts& part, int Hq, int hd, int ctas, uint16_t* out, cudaStream_t st);
 
 }  // namespace sol

@@ -34,8 +34,7 @@ struct RowsDev {
   const uint64_t* mask;  // [B][max_nodes]; nullptr: a decode step
   const uint16_t* q;     // [B][max_nodes][Hq][HD]
   uint16_t* out;
-  float* part;           // [2 gridDim.x][part_rows][HD + 2]: sums, maximum (base 2), sum of the weights
-  int part_rows;         // query rows a chain has at most
+  ChainParts part;       // 2 slots per CTA
   float* logits;         // decode steps with weights: [B][Hkv][G][Tmax] base-2 logits, else nullptr
   float* lse;            // ... [B][Hq] base-2 log of the weights' sum (infinite where no token counts), of chains that were not cut
   int* status;
@@ -59,7 +58,10 @@ template <int HD>
 __device__ __forceinline__ uint32_t ra_piece(uint32_t base, int r, int c) {
   return base + (uint32_t)((c >> 3) * RaSize<HD>::HALF + r * 128 + (((c & 7) ^ (r & 7)) << 4));
 }
-__device__ __forceinline__ void ra_consumer_sync() { asm volatile("bar.sync 1, %0;" ::"n"(RA_WARPS * 32) : "memory"); }
+__device__ __forceinline__ void ra_consumer_sync() {
+  __syncwarp();
+  asm volatile("bar.sync 1, %0;" ::"n"(RA_WARPS * 32) : "memory");
+}
 
 template <int HD>
 __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_constant__ CUtensorMap kmap,
@@ -101,7 +103,12 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
           int page = __shfl_sync(0xffffffffu, mine, x / Z::STEPS);
           // step `it` goes to warp it % RA_WARPS, whose use number `use` of its ring it is
           const int use = it / RA_WARPS, st = it % RA_WARPS * RA_DEPTH + use % RA_DEPTH;
-          if (use >= RA_DEPTH && !mbar_wait(&empty[st], (use / RA_DEPTH - 1) & 1, p.status)) return;  // the consumers give up too
+          if (use >= RA_DEPTH && !__all_sync(0xffffffffu, mbar_wait(&empty[st], (use / RA_DEPTH - 1) & 1, p.status))) {
+            // the consumers give up too; what has been requested still arrives before the CTA ends
+            for (int i = max(0, it - Z::STAGES); i < it; ++i)
+              mbar_wait(&full[i % RA_WARPS * RA_DEPTH + i / RA_WARPS % RA_DEPTH], (i / RA_WARPS / RA_DEPTH) & 1, p.status);
+            return;
+          }
           if (lane == 0) {
             const bool ok = page >= 0 && page < p.c.kv.num_pages;
             if (!ok) {
@@ -159,7 +166,7 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
     for (int x = (warp - it % RA_WARPS + RA_WARPS) % RA_WARPS; x < len; x += RA_WARPS) {
       const int use = (it + x) / RA_WARPS, st = warp * RA_DEPTH + use % RA_DEPTH;
       const int tok0 = c.tile0 * PAGE + x * Z::TOK;  // first token of the step
-      alive = alive && mbar_wait(&full[st], (use / RA_DEPTH) & 1, p.status);
+      alive = alive && __all_sync(0xffffffffu, mbar_wait(&full[st], (use / RA_DEPTH) & 1, p.status));
       if (!alive) break;
       const uint32_t kb = smem_u32(ring + (size_t)st * 2 * Z::TILE), vb = kb + Z::TILE;
       const bool ok = page_ok[st] != 0;
@@ -352,7 +359,7 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
         l1 += __shfl_xor_sync(0xffffffffu, l1, off);
       }
       const bool whole = c.whole();
-      float* part = p.part + (size_t)(2 * blockIdx.x + (u > u0)) * p.part_rows * (HD + 2);
+      const size_t part = (size_t)(2 * blockIdx.x + (u > u0)) * p.part.rows + g;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int r = r0 + 8 * h;
@@ -365,11 +372,11 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
             *reinterpret_cast<uint32_t*>(p.out + base[h] + j * 8 + 2 * t) = pack_bf16(o[j][2 * h] * inv, o[j][2 * h + 1] * inv);
           if (p.lse && t == 0) p.lse[(size_t)c.b * p.Hq + c.kvh * G + r] = l == 0.f ? INFINITY : m + log2f(l);
         } else {
-          float* dst = part + (size_t)(g + 8 * h) * (HD + 2);
+          float* dst = p.part.sums + (part + 8 * h) * HD;
 #pragma unroll
           for (int j = 0; j < ND; ++j)
             *reinterpret_cast<float2*>(dst + j * 8 + 2 * t) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
-          if (t == 0) *reinterpret_cast<float2*>(dst + HD) = make_float2(m, l);
+          if (t == 0) p.part.ml[part + 8 * h] = make_float2(m, l);
         }
       }
     }
@@ -379,73 +386,34 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
 
 // ---- merge of the chains that were cut -----------------------------------------------------------
 constexpr int RM_THREADS = 256;
-
-// Factors of a chain's pieces: row r of piece i counts 2^(m_i - M) / sum_i l_i 2^(m_i - M).  fac: [pieces][rows].  By the whole
-// CTA; a warp takes a row at a time.  lse (optional): base-2 log of the row's sum.
-__device__ __forceinline__ void chain_factors(const ChainCut& cut, const float* part, int part_rows, int stride, int rows, float* fac,
-                                              float* lse) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, np = cut.pieces();
-  for (int r = warp; r < rows; r += blockDim.x >> 5) {
-    auto ml = [&](int i) {
-      return *reinterpret_cast<const float2*>(part + ((size_t)cut.slot(i) * part_rows + r) * stride + stride - 2);
-    };
-    float m = -INFINITY;
-    for (int i = lane; i < np; i += 32) m = fmaxf(m, ml(i).x);
-    m = warp_max(m);
-    const float base = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    for (int i = lane; i < np; i += 32) {
-      const float2 v = ml(i);
-      l += v.y * exp2f(v.x - base);
-    }
-    l = warp_sum(l);
-    const float inv = l == 0.f ? 0.f : 1.0f / l;  // a row that sees nothing
-    for (int i = lane; i < np; i += 32) fac[(size_t)i * rows + r] = exp2f(ml(i).x - base) * inv;
-    if (lse && lane == 0) lse[r] = l == 0.f ? INFINITY : base + log2f(l);
-  }
-}
+constexpr int RM_ROWS = RM_THREADS / 16;  // rows of a CTA, 16 lanes each
 
 template <int HD>
-__device__ __forceinline__ void chain_merge(const RowsDev& p, const ChainCut& cut, const float* fac, int rows, int b, int kvh, int block) {
-  const int np = cut.pieces();
-  for (int e = (int)threadIdx.x * 2; e < rows * HD; e += RM_THREADS * 2) {
-    const int r = e / HD, d = e - r * HD;
-    float2 a = make_float2(0.f, 0.f);
-#pragma unroll 8
-    for (int i = 0; i < np; ++i) {
-      const float2 v = *reinterpret_cast<const float2*>(p.part + ((size_t)cut.slot(i) * p.part_rows + r) * (HD + 2) + d);
-      const float f = fac[(size_t)i * rows + r];
-      a.x += f * v.x;
-      a.y += f * v.y;
-    }
-    const int row = block * RA_ROWS + r, node = row / p.c.G;
-    *reinterpret_cast<uint32_t*>(p.out + (((size_t)b * p.c.max_nodes + node) * p.Hq + kvh * p.c.G + (row - node * p.c.G)) * HD + d) =
-        pack_bf16(a.x, a.y);
-  }
-}
-
-template <int HD>
-__global__ void __launch_bounds__(RM_THREADS) rows_merge_kernel(const RowsDev p, int ctas) {
-  extern __shared__ float rm_fac[];  // [pieces of a chain][RA_ROWS]
+__global__ void __launch_bounds__(RM_THREADS) chain_merge_kernel(const ChainShape c, const ChainParts part, int Hq, int ctas,
+                                                                 uint16_t* __restrict__ out) {
   __shared__ ChainPlan plan;
   pdl_trigger();
-  chain_plan(p.c, plan, nullptr);
-  const int run = chain_run(p.c, plan, ctas);
+  chain_plan(c, plan, nullptr);
+  const int run = chain_run(c, plan, ctas);
   pdl_wait();
-  const int kvh = blockIdx.x;
-  for (int b = blockIdx.y; b < p.c.B; b += gridDim.y) {
-    const ChainSeq s = plan.seq[b];
-    const int blocks = s.n > 0 ? chain_blocks(p.c, s) : 0;
-    for (int block = blockIdx.z; block < blocks; block += gridDim.z) {
-      const ChainCut cut = chain_cut(p.c, plan, run, b, kvh * blocks + block);
-      if (!cut.cut()) continue;
-      const int rows = min(RA_ROWS, s.n * p.c.G - block * RA_ROWS);
-      __syncthreads();
-      chain_factors(cut, p.part, p.part_rows, HD + 2, rows, rm_fac, nullptr);
-      __syncthreads();
-      chain_merge<HD>(p, cut, rm_fac, rows, b, kvh, block);
-    }
-  }
+  const int kvh = blockIdx.x, b = blockIdx.y, row = blockIdx.z * RM_ROWS + (threadIdx.x >> 4);
+  const ChainSeq s = plan.seq[b];
+  const int blocks = chain_blocks(c, s), block = blockIdx.z * RM_ROWS / c.block_rows, rows = s.n * c.G;
+  if (block >= blocks) return;
+  const ChainCut cut = chain_cut(c, plan, run, b, kvh * blocks + block);
+  if (!cut.cut()) return;
+  const int local = min(row, rows - 1) - block * c.block_rows;  // whole warps take part in the reductions
+  const float2 ml = chain_merged_ml(part, cut, local);
+  const int node = row / c.G;
+  if (row < rows)
+    chain_merged_row<HD>(part, cut, local, ml, out + (((size_t)b * c.max_nodes + node) * Hq + kvh * c.G + (row - node * c.G)) * HD);
+}
+
+// After an attention kernel of `ctas` CTAs that left its cut chains in `part`.
+void launch_chain_merge(const ChainShape& c, const ChainParts& part, int Hq, int hd, int ctas, uint16_t* out, cudaStream_t st) {
+  const dim3 grid(c.Hkv, c.B, (c.max_nodes * c.G + RM_ROWS - 1) / RM_ROWS);
+  if (hd == 64) SOL_LAUNCH("chain_merge", chain_merge_kernel<64>, grid, dim3(RM_THREADS), 0, st, c, part, Hq, ctas, out);
+  else SOL_LAUNCH("chain_merge", chain_merge_kernel<128>, grid, dim3(RM_THREADS), 0, st, c, part, Hq, ctas, out);
 }
 
 // ---- the weights of a decode step ----------------------------------------------------------------
@@ -453,9 +421,8 @@ constexpr int WK_TOKENS = RM_THREADS * 4;  // tokens of a unit
 
 template <int HD>
 __global__ void __launch_bounds__(RM_THREADS) weight_kernel(const RowsDev p, int ctas, float decay, float* __restrict__ weights) {
-  extern __shared__ float wk_fac[];
   __shared__ ChainPlan plan;
-  __shared__ float lse[8];
+  __shared__ float lse[RM_ROWS];
   __shared__ int units[CHAIN_MAX_BATCH + 1];
   const int tid = threadIdx.x;
   pdl_trigger();
@@ -483,10 +450,17 @@ __global__ void __launch_bounds__(RM_THREADS) weight_kernel(const RowsDev p, int
     const int kvh = (u - units[b]) / per, chunk = (u - units[b]) - kvh * per;
     const ChainCut cut = chain_cut(p.c, plan, run, b, kvh);
     __syncthreads();
-    if (cut.cut()) chain_factors(cut, p.part, p.part_rows, HD + 2, G, wk_fac, lse);
-    else if (tid < G) lse[tid] = p.lse[(size_t)b * p.Hq + kvh * G + tid];
+    if (cut.cut()) {
+      const int g = tid >> 4;
+      if (g < (G + 1) / 2 * 2) {  // whole warps
+        const float2 ml = chain_merged_ml(p.part, cut, min(g, G - 1));
+        if (g < G && chunk == 0) chain_merged_row<HD>(p.part, cut, g, ml, p.out + ((size_t)b * p.Hq + kvh * G + g) * HD);
+        if (g < G && (tid & 15) == 0) lse[g] = ml.y == 0.f ? INFINITY : ml.x + log2f(ml.y);
+      }
+    } else if (tid < G) {
+      lse[tid] = p.lse[(size_t)b * p.Hq + kvh * G + tid];
+    }
     __syncthreads();
-    if (chunk == 0 && cut.cut()) chain_merge<HD>(p, cut, wk_fac, G, b, kvh, 0);
     const int tok = chunk * WK_TOKENS + tid * 4;
     if (tok >= T) continue;
     const size_t bk = (size_t)b * p.c.Hkv + kvh;
@@ -506,21 +480,18 @@ __global__ void __launch_bounds__(RM_THREADS) weight_kernel(const RowsDev p, int
 }
 
 // ---- host ----------------------------------------------------------------------------------------
-size_t rows_part_bytes(const sol_shape_t& sh) { return (size_t)2 * sm_count() * RA_ROWS * (sh.head_dim + 2) * 4; }
+size_t rows_part_bytes(const sol_shape_t& sh) { return chain_part_bytes(sm_count(), RA_ROWS, sh.head_dim); }
 
 template <int HD>
-static void launch_rows(const RowsDev& d, const CUtensorMap& kmap, const CUtensorMap& vmap, const RowsArgs& a, cudaStream_t st) {
+static void launch_rows(RowsDev d, const CUtensorMap& kmap, const CUtensorMap& vmap, const RowsArgs& a, cudaStream_t st) {
   // fewer CTAs where the caller's space for partial results is short
-  const int ctas = (int)std::min<size_t>(sm_count(), a.part_bytes / ((size_t)2 * d.part_rows * (HD + 2) * 4));
+  const int rows = a.weights ? d.c.G : RA_ROWS;
+  const int ctas = (int)std::min<size_t>(sm_count(), a.part_bytes / chain_part_bytes(1, rows, HD));
+  d.part = chain_parts(a.part, ctas, rows, HD);
   ensure_dynamic_smem(reinterpret_cast<const void*>(&rows_attn_kernel<HD>), RaSize<HD>::SMEM);
   SOL_LAUNCH("rows_attn", rows_attn_kernel<HD>, dim3(ctas), dim3(RA_THREADS), RaSize<HD>::SMEM, st, kmap, vmap, d);
-  const int fac = ctas * RA_ROWS * 4;
-  if (a.weights) {
-    SOL_LAUNCH("attn_weights", weight_kernel<HD>, dim3(4 * ctas), dim3(RM_THREADS), fac, st, d, ctas, a.decay, a.weights);
-  } else {
-    const int blocks = (a.max_nodes * d.c.G + RA_ROWS - 1) / RA_ROWS;
-    SOL_LAUNCH("rows_merge", rows_merge_kernel<HD>, dim3(d.c.Hkv, d.c.B, blocks), dim3(RM_THREADS), fac, st, d, ctas);
-  }
+  if (a.weights) SOL_LAUNCH("attn_weights", weight_kernel<HD>, dim3(4 * ctas), dim3(RM_THREADS), 0, st, d, ctas, a.decay, a.weights);
+  else launch_chain_merge(d.c, d.part, d.Hq, HD, ctas, d.out, st);
 }
 
 void launch_rows_attention(const RowsArgs& a, cudaStream_t st) {
@@ -528,24 +499,16 @@ void launch_rows_attention(const RowsArgs& a, cudaStream_t st) {
   CUtensorMap kmap, vmap;
   const int box = sh.head_dim == 64 ? RaSize<64>::TOK : RaSize<128>::TOK;
   if (!encode_pool_map(&kmap, a.kv.k_pool, sh, a.kv.num_pages, box) ||
-      !encode_pool_map(&vmap, a.kv.v_pool, sh, a.kv.num_pages, box)) return;
+      !encode_pool_map(&vmap, a.kv.v_pool, sh, a.kv.num_pages, box))
+    return;
   RowsDev d;
   memset(&d, 0, sizeof(d));
-  d.c.kv = a.kv;
-  d.c.B = a.B;
-  d.c.Hkv = sh.n_kv_heads;
-  d.c.G = sh.n_q_heads / sh.n_kv_heads;
-  d.c.max_nodes = a.max_nodes;
-  d.c.n_nodes = a.n_nodes;
-  d.c.block_rows = RA_ROWS;
-  d.c.min_tiles = RA_MIN_TILES;
+  d.c = chain_shape(a, RA_ROWS, PAGE, RA_MIN_TILES);
   d.Hq = sh.n_q_heads;
   d.scale_log2 = 1.4426950408889634f / sqrtf((float)sh.head_dim);
   d.mask = a.mask;
   d.q = static_cast<const uint16_t*>(a.q);
   d.out = static_cast<uint16_t*>(a.out);
-  d.part = a.part;
-  d.part_rows = a.weights ? d.c.G : RA_ROWS;
   d.logits = a.weights ? a.logits : nullptr;
   d.lse = a.weights ? a.lse : nullptr;
   d.status = a.status;
