@@ -63,7 +63,9 @@ inline ChainShape chain_shape(const RowsArgs& a, int block_rows, int tile, int m
   return c;
 }
 
-__device__ __forceinline__ int chain_tiles(const ChainShape& c, const ChainSeq& s) { return max(1, (s.T + c.tile - 1) / c.tile); }
+__device__ __forceinline__ int chain_tiles(const ChainShape& c, const ChainSeq& s) {
+  return max(1, (s.T + c.tile - 1) / (c.tile == PAGE ? PAGE : 2 * PAGE));
+}
 __device__ __forceinline__ int chain_blocks(const ChainShape& c, const ChainSeq& s) { return (s.n * c.G + c.block_rows - 1) / c.block_rows; }
 
 // By the whole CTA (128 threads at least); ends with a barrier.
@@ -133,7 +135,7 @@ __device__ __forceinline__ ChainPiece chain_piece(const ChainShape& c, const Cha
 // Where the pieces of a cut chain lie: CTAs first .. last, of which the first one's piece is in its slot 1 unless the chain
 // begins with its run; the others' are in slot 0.
 struct ChainCut {
-  int first, last, first_slot;
+  int first, last, first_slot;  // CTAs, and the first piece's slot
   __device__ __forceinline__ bool cut() const { return last > first; }
   __device__ __forceinline__ int slot(int i) const { return i == 0 ? first_slot : 2 * (first + i); }  // of piece i
   __device__ __forceinline__ int pieces() const { return last - first + 1; }
@@ -148,19 +150,47 @@ __device__ __forceinline__ ChainCut chain_cut(const ChainShape& c, const ChainPl
 }
 
 // ---- partial results of cut chains ----
+// A chain that begins in a CTA's run and goes on in the next: for the kernel that merges its pieces.
+struct ChainDesc {
+  int pieces;  // 0: there is none
+  int b, kvh, block, rows, first_slot;
+};
 // Per slot and row of a chain: HD weighted sums, and (maximum in the base-2 domain, sum of the weights).
 struct ChainParts {
-  float* sums;  // [slots][rows][HD]
-  float2* ml;   // [slots][rows]
+  float* sums;      // [slots][rows][HD]
+  float2* ml;       // [slots][rows]
+  ChainDesc* desc;  // [ctas]
   int rows;
 };
-inline size_t chain_part_bytes(int ctas, int rows, int hd) { return (size_t)2 * ctas * rows * (hd * 4 + 8); }
+inline size_t chain_part_bytes(int ctas, int rows, int hd) {
+  return (size_t)2 * ctas * rows * (hd * 4 + 8) + ctas * sizeof(ChainDesc);
+}
 inline ChainParts chain_parts(void* base, int ctas, int rows, int hd) {
   ChainParts p;
   p.sums = static_cast<float*>(base);
   p.ml = reinterpret_cast<float2*>(p.sums + (size_t)2 * ctas * rows * hd);
+  p.desc = reinterpret_cast<ChainDesc*>(p.ml + (size_t)2 * ctas * rows);
   p.rows = rows;
   return p;
+}
+
+// What CTA `cta` with run [u0, u1) of the line leaves to be merged, by one thread.
+__device__ __forceinline__ void chain_describe(const ChainShape& c, const ChainPlan& p, int run, int cta, int u0, int u1, ChainDesc* out) {
+  ChainDesc d;
+  d.pieces = d.b = d.kvh = d.block = d.rows = d.first_slot = 0;
+  if (u0 < u1) {
+    const ChainPiece last = chain_piece(c, p, u1 - 1, u1);
+    const int start = u1 - 1 - last.tile0;
+    if (last.tile0 + 1 < last.tiles && start >= u0) {
+      d.pieces = (start + last.tiles - 1) / run - cta + 1;
+      d.b = last.b;
+      d.kvh = last.kvh;
+      d.block = last.block;
+      d.rows = min(c.block_rows, last.seq.n * c.G - last.block * c.block_rows);
+      d.first_slot = 2 * cta + (start > u0);
+    }
+  }
+  out[cta] = d;
 }
 
 // A row's merged maximum and 1 / (sum of the weights) (0 for a row that sees nothing), by the 16 lanes of half a warp.

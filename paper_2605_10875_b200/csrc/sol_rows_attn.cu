@@ -90,6 +90,7 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
   const int run = chain_run(p.c, plan, gridDim.x);
   const int u0 = (int)min((long long)blockIdx.x * run, (long long)plan.cum[p.c.B]), u1 = min(plan.cum[p.c.B], u0 + run);
 
+  if (tid == 0) chain_describe(p.c, plan, run, blockIdx.x, u0, u1, p.part.desc);
   if (warp == RA_WARPS) {  // ---- the producer ----
     int it = 0;
     for (int u = u0; u < u1;) {
@@ -388,32 +389,33 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
 constexpr int RM_THREADS = 256;
 constexpr int RM_ROWS = RM_THREADS / 16;  // rows of a CTA, 16 lanes each
 
+// A CTA per (CTA of the attention kernel, 16 rows): the chain that begins in that CTA's run and goes on in the next.  The
+// attention kernel has written down which one that is: finding it again from the lengths took longer than the merge.
 template <int HD>
-__global__ void __launch_bounds__(RM_THREADS) chain_merge_kernel(const ChainShape c, const ChainParts part, int Hq, int ctas,
+__global__ void __launch_bounds__(RM_THREADS) chain_merge_kernel(const ChainParts part, int G, int max_nodes, int Hq, int block_rows,
                                                                  uint16_t* __restrict__ out) {
-  __shared__ ChainPlan plan;
   pdl_trigger();
-  chain_plan(c, plan, nullptr);
-  const int run = chain_run(c, plan, ctas);
   pdl_wait();
-  const int kvh = blockIdx.x, b = blockIdx.y, row = blockIdx.z * RM_ROWS + (threadIdx.x >> 4);
-  const ChainSeq s = plan.seq[b];
-  const int blocks = chain_blocks(c, s), block = blockIdx.z * RM_ROWS / c.block_rows, rows = s.n * c.G;
-  if (block >= blocks) return;
-  const ChainCut cut = chain_cut(c, plan, run, b, kvh * blocks + block);
-  if (!cut.cut()) return;
-  const int local = min(row, rows - 1) - block * c.block_rows;  // whole warps take part in the reductions
-  const float2 ml = chain_merged_ml(part, cut, local);
-  const int node = row / c.G;
-  if (row < rows)
-    chain_merged_row<HD>(part, cut, local, ml, out + (((size_t)b * c.max_nodes + node) * Hq + kvh * c.G + (row - node * c.G)) * HD);
+  const ChainDesc d = part.desc[blockIdx.x];
+  if (blockIdx.y * RM_ROWS >= d.rows || d.pieces == 0) return;
+  ChainCut cut;
+  cut.first = blockIdx.x;
+  cut.last = blockIdx.x + d.pieces - 1;
+  cut.first_slot = d.first_slot;
+  const int row = blockIdx.y * RM_ROWS + (threadIdx.x >> 4);
+  const float2 ml = chain_merged_ml(part, cut, min(row, d.rows - 1));  // whole warps take part in the reductions
+  if (row >= d.rows) return;
+  const int r = d.block * block_rows + row, node = r / G;
+  chain_merged_row<HD>(part, cut, row, ml, out + (((size_t)d.b * max_nodes + node) * Hq + d.kvh * G + (r - node * G)) * HD);
 }
 
 // After an attention kernel of `ctas` CTAs that left its cut chains in `part`.
 void launch_chain_merge(const ChainShape& c, const ChainParts& part, int Hq, int hd, int ctas, uint16_t* out, cudaStream_t st) {
-  const dim3 grid(c.Hkv, c.B, (c.max_nodes * c.G + RM_ROWS - 1) / RM_ROWS);
-  if (hd == 64) SOL_LAUNCH("chain_merge", chain_merge_kernel<64>, grid, dim3(RM_THREADS), 0, st, c, part, Hq, ctas, out);
-  else SOL_LAUNCH("chain_merge", chain_merge_kernel<128>, grid, dim3(RM_THREADS), 0, st, c, part, Hq, ctas, out);
+  const dim3 grid(ctas, (part.rows + RM_ROWS - 1) / RM_ROWS);
+  if (hd == 64)
+    SOL_LAUNCH("chain_merge", chain_merge_kernel<64>, grid, dim3(RM_THREADS), 0, st, part, c.G, c.max_nodes, Hq, c.block_rows, out);
+  else
+    SOL_LAUNCH("chain_merge", chain_merge_kernel<128>, grid, dim3(RM_THREADS), 0, st, part, c.G, c.max_nodes, Hq, c.block_rows, out);
 }
 
 // ---- the weights of a decode step ----------------------------------------------------------------

@@ -3,18 +3,22 @@
 //
 //   o_r = sum_t p_rt v_t,  p_rt = 2^(s_rt - m_r) / l_r,  s_rt = (q_r . k_t) log2(e) / sqrt(head_dim)  where row r sees token t
 //
-// One CTA per SM takes its run of tiles (sol_chain.cuh; a tile is two cache pages, 128 tokens), cut chains are merged by
-// chain_merge_kernel.  Two units of 128 rows work on it, each with scores (128 columns) and sums (head_dim columns) in tensor
-// memory: blocks of more than 128 rows give each unit its own rows and both read every tile; smaller ones give both units the
-// same rows and every second tile, and the units' results are merged at the end of the chain.  So one unit's products run
-// while the other's softmax does.
+// One CTA per SM takes its run of tiles (sol_chain.cuh; a tile is two cache pages of one kv-head, 128 tokens), cut chains are
+// merged by chain_merge_kernel.  Two units of 128 tensor-memory lanes work on it, each with scores (128 columns) and sums
+// (head_dim columns): while one unit's softmax runs, the other's products do.  Blocks of more than 128 query rows give each unit
+// its own rows, and both read every tile; smaller ones give both units the same rows and every second tile.  Up to 64 (32) rows
+// are there twice (four times) in a unit's lanes, so that each copy weighs only half (a quarter) of a tile's tokens and the
+// softmax uses all four of the SM's quarters.  What the units and the copies have is added up at the end of a piece.
 //
-//   warps 0-3, 4-7   the units' softmax, a row per thread: scores from tensor memory, running maximum (moved only where it
+//   warps 0-3, 4-7   the units' softmax, a lane per thread: scores from tensor memory, running maximum (moved only where it
 //                    grows by more than 2^8: then the sums are rescaled), weights as bf16 back to where the scores were
-//   warp 8           TMA of keys and values into a ring of 128-token operand tiles (128-byte swizzle)
-//   warp 9           tcgen05.mma: S = Q K^T (both from shared memory), O += P V (P from tensor memory)
-//   warps 10, 11     clear rows of a tile that no weight may meet: behind the sequence, of a page out of range, and of drafted
-//                    tokens with values that are not finite, which the softmax threads add in float32 for the rows that see them
+//   warps 8, 9       TMA of keys, of values into a ring each of 128-token operand tiles (128-byte swizzle)
+//   warp 10          tcgen05.mma: S = Q K^T (both from shared memory), O += P V (P from tensor memory)
+//   warp 11          clears rows of values that no weight may meet: behind the sequence, and of drafted tokens that are not finite,
+//                    which the softmax threads add in float32 for the rows that see them
+//
+// Code that runs once a piece is kept short (rolled loops, rare work in functions of their own): fetched cold, it took longer
+// than the piece's end does.
 #include <cuda.h>
 #include <math.h>
 
@@ -25,22 +29,26 @@
 
 namespace sol {
 
-constexpr int TA_ROWS = 128;            // rows of a unit
+constexpr int TA_ROWS = 128;            // lanes of a unit
 constexpr int TA_BLOCK = 2 * TA_ROWS;   // rows of a chain
 constexpr int TA_TILE = 2 * PAGE;       // tokens of a tile
 constexpr int TA_MIN_TILES = 2;
 constexpr int TA_THREADS = 12 * 32;
 constexpr float TA_SLACK = 8.f;         // weights reach 2^8 before the maximum moves
-enum : int { TAW_LOAD = 8, TAW_MMA = 9, TAW_CLEAR = 10 };
+constexpr int TA_EX = 32;               // columns handed over at a time at the end of a piece
+enum : int { TAW_KEYS = 8, TAW_VALUES = 9, TAW_MMA = 10, TAW_CLEAR = 11 };
 
 template <int HD>
 struct TaSize {
   static constexpr int CHUNKS = HD / 64;
-  static constexpr int CHUNK = 128 * 128;         // a 64-wide chunk of an operand: [128 rows][128 B]
-  static constexpr int OPER = CHUNKS * CHUNK;     // queries of a unit, keys or values of a tile
-  static constexpr int SLOTS = HD == 64 ? 12 : 5;
-  static constexpr int SMEM = 1024 + (2 + SLOTS) * OPER;
-  static constexpr int UNIT = TA_TILE + HD;       // tensor-memory columns of a unit
+  static constexpr int CHUNK = 128 * 128;        // a 64-wide chunk of an operand: [128 rows][128 B]
+  static constexpr int OPER = CHUNKS * CHUNK;    // a unit's queries, a tile's keys or values
+  static constexpr int K_SLOTS = HD == 64 ? 5 : 2, V_SLOTS = HD == 64 ? 6 : 3;
+  static constexpr int RINGS = (K_SLOTS + V_SLOTS) * OPER;
+  static constexpr int EX = HD == 64 ? 0 : OPER;                        // where columns of sums are handed over: [TA_EX][256]
+  static constexpr int ML = HD == 64 ? 2 * OPER + RINGS : 0;            // ... maxima and sums of weights: [256]
+  static constexpr int SMEM = 1024 + 2 * OPER + RINGS + (HD == 64 ? 256 * 8 : 0);
+  static constexpr int UNIT = TA_TILE + HD;      // columns of a unit: scores, sums
 };
 
 struct TreeDev {
@@ -54,22 +62,25 @@ struct TreeDev {
   int* status;
 };
 
-struct TreeClearJob {  // from the MMA warp to the clearing warps
-  int slot, base, C, T, pages, units, quit;
+constexpr int TA_JOBS = 8;  // two of a piece that ends, and as many as there are slots for values
+struct TreeClearJob {       // from the values' warp to the clearing warp
+  int slot, phase, base, C, T;  // slot < 0: that was all
 };
 
 template <int HD>
 struct TreeShared {
   ChainPlan plan;
-  uint64_t full[TaSize<HD>::SLOTS], empty[TaSize<HD>::SLOTS];
-  uint64_t q_ready[2], s_full[2], p_ready[2], o_done[2], go, clean;
-  unsigned long long dirty[2];  // per unit: drafted tokens whose values were taken out
-  TreeClearJob job;
+  uint64_t k_full[TaSize<HD>::K_SLOTS], k_empty[TaSize<HD>::K_SLOTS];
+  uint64_t v_full[TaSize<HD>::V_SLOTS], v_empty[TaSize<HD>::V_SLOTS], v_clean[TaSize<HD>::V_SLOTS];
+  uint64_t q_ready, s_full[2], p_ready[2], o_end[2];
+  TreeClearJob jobs[TA_JOBS];
+  unsigned long long dirty[TA_JOBS];  // per job: drafted tokens whose values were taken out
+  int posted;                         // jobs so far
   uint32_t tmem;
-  unsigned char pages[TaSize<HD>::SLOTS];  // bit i: page i of the tile is there
 };
 
-__device__ __forceinline__ uint32_t ta_piece(uint32_t oper, int r, int c) {  // address of 16-byte piece c of row r of an operand
+// Address of 16-byte piece c of row r of an operand.
+__device__ __forceinline__ uint32_t ta_piece(uint32_t oper, int r, int c) {
   return oper + (uint32_t)((c >> 3) * (128 * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4));
 }
 __device__ __forceinline__ float ta_exp2(float x) {
@@ -78,10 +89,33 @@ __device__ __forceinline__ float ta_exp2(float x) {
   return y;
 }
 
+__device__ __forceinline__ float ta_max3(float a, float b, float c) {  // of numbers: NaN loses
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+__device__ __forceinline__ uint32_t ta_pack(float lo, float hi) {
+  uint32_t y;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
+  return y;
+}
+__device__ __forceinline__ uint64_t ta_add2(uint64_t a, uint64_t b) {
+  uint64_t y;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+  return y;
+}
+__device__ __forceinline__ float2 ta_unpack2(uint64_t a) {
+  float2 y;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(y.x), "=f"(y.y) : "l"(a));
+  return y;
+}
+
 // What a piece of a chain means to every role.
 struct TreePiece : ChainPiece {
   int rows, steps, C;  // query rows of the block, tiles of the piece, tokens of the committed context
   bool both;           // both units read every tile
+  int lanes;           // lanes of a copy of the rows
+  __device__ __forceinline__ int first_mixed() const { return max(tile0, C / TA_TILE); }  // from here on: drafted tokens, the end
 };
 __device__ __forceinline__ TreePiece tree_piece(const ChainShape& c, const ChainPlan& plan, int u, int end) {
   TreePiece r;
@@ -90,233 +124,272 @@ __device__ __forceinline__ TreePiece tree_piece(const ChainShape& c, const Chain
   r.steps = r.tile1 - r.tile0;
   r.C = r.seq.T - r.seq.n;
   r.both = r.rows > TA_ROWS;
+  r.lanes = r.rows > 64 ? 128 : r.rows > 32 ? 64 : 32;
   return r;
 }
 
-// ---- TMA ----
-template <int HD>
-__device__ void tree_load(const TreeDev& p, TreeShared<HD>& sh, unsigned char* ring, const CUtensorMap* kmap, const CUtensorMap* vmap,
-                          int u0, int u1) {
+// ---- TMA, a warp for the keys and one for the values ----
+// A page out of range is reported and not read: no row sees its tokens, and its values are zeros.  Tiles of values that need it are
+// handed to the clearing warp as soon as they are on their way.
+template <int HD, bool VALUES>
+__device__ void tree_load(const TreeDev& p, TreeShared<HD>& sh, unsigned char* ring, const CUtensorMap* map, int u0, int u1) {
   using Z = TaSize<HD>;
+  constexpr int SLOTS = VALUES ? Z::V_SLOTS : Z::K_SLOTS;
+  uint64_t *full = VALUES ? sh.v_full : sh.k_full, *empty = VALUES ? sh.v_empty : sh.k_empty;
   const int lane = threadIdx.x & 31;
   bool alive = true;
-  int n = 0;  // tiles requested so far
+  int slot = 0, n = 0, jobs = 0;  // slot of the next tile; tiles, jobs so far
+  uint32_t phase = 1;             // of the slot's `empty`: a fresh barrier counts as having completed the phase before its first
   for (int u = u0; u < u1;) {
     const TreePiece c = tree_piece(p.c, sh.plan, u, u1);
-    const int32_t* table = p.c.kv.page_table + (size_t)c.b * p.c.kv.max_pages_per_seq;
-    const int pages = (c.seq.T + PAGE - 1) / PAGE;
-    // page numbers of 16 steps at a time, the next 16 requested two steps after the last ones came into use (values come one
-    // step after keys, so both sets are in use for a while)
-    int win[2];
-    auto fetch = [&](int w) {
-      const int i = 2 * (c.tile0 + 16 * w) + lane;
-      return i < pages && i < 2 * c.tile1 ? table[i] : -1;
-    };
-    win[0] = fetch(0);
-    win[1] = c.steps > 16 ? fetch(1) : -1;
-    auto push = [&](const CUtensorMap* map, int step) {
-      const int w = win[(step >> 4) & 1], at = 2 * (step & 15);
-      const int page0 = __shfl_sync(0xffffffffu, w, at), page1 = __shfl_sync(0xffffffffu, w, at + 1);
-      const int slot = n % Z::SLOTS, use = n / Z::SLOTS;
-      if (alive && use > 0) alive = __all_sync(0xffffffffu, mbar_wait(&sh.empty[slot], (use - 1) & 1, p.status));
-      if (!alive) return;
-      ++n;
-      if (lane == 0) {
-        const int tile = c.tile0 + step;
-        const int ids[2] = {page0, page1};
-        int there = 0;
-        for (int x = 0; x < 2; ++x) {
-          if (2 * tile + x >= pages) continue;
-          if (ids[x] >= 0 && ids[x] < p.c.kv.num_pages) there |= 1 << x;
-          else atomicOr(p.status + ST_ERR, ERR_BAD_PAGE);
+    const int pages = (c.seq.T + PAGE - 1) / PAGE - 2 * c.tile0;  // of the sequence, from the piece's first on
+    const int32_t* table = p.c.kv.page_table + (size_t)c.b * p.c.kv.max_pages_per_seq + 2 * c.tile0;
+    const int last = min(pages, 2 * c.steps);
+    int now = 0, next = lane < last ? table[lane] : -1;  // page numbers, 32 at a time
+#pragma unroll 1
+    for (int j = 0; j < c.steps; ++j) {
+      if ((j & 15) == 0) {
+        now = next;
+        next = 2 * j + 32 + lane < last ? table[2 * j + 32 + lane] : -1;
+      }
+      const int id0 = __shfl_sync(0xffffffffu, now, 2 * j & 31), id1 = __shfl_sync(0xffffffffu, now, 2 * j + 1 & 31);
+      alive = alive && __all_sync(0xffffffffu, mbar_wait(&empty[slot], phase, p.status));
+      if (!alive) continue;
+      unsigned char* dst = ring + (size_t)slot * Z::OPER;
+      const bool two = 2 * j + 1 < pages, good0 = id0 >= 0 && id0 < p.c.kv.num_pages, good1 = two && id1 >= 0 && id1 < p.c.kv.num_pages;
+      if (!good0 || (two && !good1)) {
+        for (int i = lane; i < Z::OPER / 16; i += 32) {
+          const bool second = (i >> 9) & 1;  // 16-byte pieces: the second page's half of a chunk
+          if (second ? two && !good1 : !good0) reinterpret_cast<uint4*>(dst)[i] = make_uint4(0u, 0u, 0u, 0u);
         }
-        sh.pages[slot] = (unsigned char)there;
-        const int parts = (there & 1) + (there >> 1);
-        if (parts == 0) {
-          mbar_arrive(&sh.full[slot]);
-        } else {
-          mbar_expect_tx(&sh.full[slot], (uint32_t)parts * (Z::OPER / 2));
-          for (int x = 0; x < 2; ++x) {
-            if (!((there >> x) & 1)) continue;
-            const int row = (ids[x] * p.c.Hkv + c.kvh) * PAGE;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        if (lane == 0) atomicOr(p.status + ST_ERR, ERR_BAD_PAGE);
+        __syncwarp();
+      }
+      if (lane == 0) {
+        uint64_t* bar = &full[slot];
+        const int bytes = ((int)good0 + (int)good1) * (Z::OPER / 2);
+        if (bytes) mbar_expect_tx(bar, bytes);
+        else mbar_arrive(bar);
 #pragma unroll
-            for (int h = 0; h < Z::CHUNKS; ++h)
-              tma_load_2d(ring + (size_t)slot * Z::OPER + h * Z::CHUNK + x * (PAGE * 128), map, h * 64, row, &sh.full[slot]);
-          }
+        for (int h = 0; h < Z::CHUNKS; ++h) {
+          if (good0) tma_load_2d(dst + h * Z::CHUNK, map, h * 64, (id0 * p.c.Hkv + c.kvh) * PAGE, bar);
+          if (good1) tma_load_2d(dst + h * Z::CHUNK + Z::CHUNK / 2, map, h * 64, (id1 * p.c.Hkv + c.kvh) * PAGE, bar);
+        }
+        if (VALUES && c.tile0 + j >= c.first_mixed()) {
+          TreeClearJob job;
+          job.slot = slot; job.phase = phase ^ 1; job.base = (c.tile0 + j) * TA_TILE; job.C = c.C; job.T = c.seq.T;
+          sh.jobs[jobs % TA_JOBS] = job;
+          __threadfence_block();
+          *const_cast<volatile int*>(&sh.posted) = ++jobs;
         }
       }
       __syncwarp();
-    };
-    auto turn = [&](int step) {  // keys of `step` have been pushed
-      if ((step & 15) == 2 && step > 16) win[((step >> 4) + 1) & 1] = fetch((step >> 4) + 1);
-    };
-    if (c.both) {
-      for (int j = 0; j < c.steps; ++j) {
-        push(kmap, j);
-        push(vmap, j);
-        turn(j);
-      }
-    } else {
-      push(kmap, 0);
-      for (int j = 0; j < c.steps; ++j) {
-        if (j + 1 < c.steps) {
-          push(kmap, j + 1);
-          turn(j + 1);
-        }
-        push(vmap, j);
+      ++n;
+      if (++slot == SLOTS) {
+        slot = 0;
+        phase ^= 1;
       }
     }
     u += c.steps;
   }
   if (!alive)  // a wait gave up: what has been requested still arrives before the CTA ends
-    for (int i = max(0, n - Z::SLOTS); i < n; ++i) mbar_wait(&sh.full[i % Z::SLOTS], (i / Z::SLOTS) & 1, p.status);
-}
-
-// ---- tensor cores ----
-template <int HD>
-__device__ void tree_mma(const TreeDev& p, TreeShared<HD>& sh, uint32_t q_oper, uint32_t ring, int u0, int u1) {
-  using Z = TaSize<HD>;
-  constexpr uint32_t S_IDESC = umma_idesc_bf16_m128(TA_TILE, 0, 0), O_IDESC = umma_idesc_bf16_m128(HD, 0, 1);
-  const uint32_t tmem = sh.tmem;
-  bool alive = true;
-  auto wait = [&](uint64_t* bar, uint32_t parity) {  // after one that gave up, the others return at once
-    alive = alive && mbar_wait(bar, parity, p.status);
-    __syncwarp();
-  };
-  int n = 0, piece = 0, jobs = 0;
-  int done[2] = {0, 0};  // steps whose weights have been waited for
-  for (int u = u0; u < u1; ++piece) {
-    const TreePiece c = tree_piece(p.c, sh.plan, u, u1);
-    wait(&sh.q_ready[0], piece & 1);
-    wait(&sh.q_ready[1], piece & 1);
-    tc_fence_after();
-    auto slot_full = [&]() {  // the next tile of the ring
-      const int slot = n % Z::SLOTS;
-      wait(&sh.full[slot], (n / Z::SLOTS) & 1);
-      ++n;
-      return slot;
-    };
-    auto scores = [&](int slot, int unit, bool last) {
-      tc_fence_after();
-      if (elect_one()) {
-        const uint32_t a = q_oper + (c.both && unit ? Z::OPER : 0), b = ring + slot * Z::OPER;
-#pragma unroll
-        for (int k = 0; k < HD / 16; ++k) {
-          const uint32_t off = (k >> 2) * Z::CHUNK + (k & 3) * 32;
-          umma_bf16(tmem + unit * Z::UNIT, umma_smem_desc(a + off, 16, 1024), umma_smem_desc(b + off, 16, 1024), S_IDESC, k > 0);
-        }
-        umma_commit(&sh.s_full[unit]);
-        if (last) umma_commit(&sh.empty[slot]);
-      }
-      __syncwarp();
-    };
-    auto values_ready = [&](int slot, int step) {  // where rows have to be cleared first, that is asked for
-      const int base = (c.tile0 + step) * TA_TILE, there = sh.pages[slot];
-      if (base + TA_TILE <= c.C && there == 3) return;
-      if ((threadIdx.x & 31) == 0) {
-        TreeClearJob j;
-        j.slot = slot; j.base = base; j.C = c.C; j.T = c.seq.T; j.pages = there;
-        j.units = c.both ? 3 : 1 << (step & 1);
-        j.quit = 0;
-        sh.job = j;
-        mbar_arrive(&sh.go);
-      }
-      __syncwarp();
-      wait(&sh.clean, jobs & 1);
-      ++jobs;
-    };
-    auto values = [&](int slot, int unit, bool fresh, bool last, bool end) {
-      wait(&sh.p_ready[unit], done[unit] & 1);
-      ++done[unit];
-      tc_fence_after();
-      if (elect_one()) {
-        const uint32_t pa = tmem + unit * Z::UNIT, b = ring + slot * Z::OPER;
-#pragma unroll
-        for (int k = 0; k < TA_TILE / 16; ++k)
-          umma_bf16_ts(pa + TA_TILE, pa + k * 8, umma_smem_desc(b + k * 2048, Z::CHUNK, 1024), O_IDESC, !fresh || k > 0);
-        if (last) umma_commit(&sh.empty[slot]);
-        if (end) {
-          umma_commit(&sh.o_done[unit]);
-          mbar_arrive(&sh.o_done[unit]);  // what this warp has seen, the unit sees: the clearing warps' finds among it
-        }
-      }
-      __syncwarp();
-    };
-    if (c.both) {
-      int slot = slot_full();
-      scores(slot, 0, false);
-      scores(slot, 1, true);
-      for (int j = 0; j < c.steps; ++j) {
-        const bool more = j + 1 < c.steps;
-        const int vs = slot_full();
-        values_ready(vs, j);
-        values(vs, 0, j == 0, false, !more);
-        if (more) {
-          slot = slot_full();
-          scores(slot, 0, false);
-        }
-        values(vs, 1, j == 0, true, !more);
-        if (more) scores(slot, 1, true);
-      }
-    } else {
-      scores(slot_full(), 0, true);
-      for (int j = 0; j < c.steps; ++j) {
-        if (j + 1 < c.steps) scores(slot_full(), (j + 1) & 1, true);
-        const int vs = slot_full();
-        values_ready(vs, j);
-        values(vs, j & 1, j < 2, true, j + 2 >= c.steps);
-      }
-    }
-    u += c.steps;
-  }
-  if ((threadIdx.x & 31) == 0) {
-    sh.job.quit = 1;
-    mbar_arrive(&sh.go);
+    for (int i = max(0, n - SLOTS); i < n; ++i) mbar_wait(&full[i % SLOTS], (i / SLOTS) & 1, p.status);
+  if (VALUES && lane == 0) {
+    sh.jobs[jobs % TA_JOBS].slot = -1;
+    __threadfence_block();
+    *const_cast<volatile int*>(&sh.posted) = ++jobs;
   }
 }
 
 // ---- rows that no weight may meet ----
 template <int HD>
-__device__ void tree_clear(const TreeDev& p, TreeShared<HD>& sh, uint32_t ring) {
+__device__ void tree_clear(const TreeDev& p, TreeShared<HD>& sh, uint32_t v_ring) {
   using Z = TaSize<HD>;
-  const int tid = threadIdx.x - TAW_CLEAR * 32;  // 0 .. 63
+  const int lane = threadIdx.x & 31;
+#pragma unroll 1
   for (int n = 0;; ++n) {
-    // the MMA warp asks seldom: wait for as long as it lives (its own waits are limited, and its last word is `quit`)
+    // there is seldom anything to do: asked for as long as the values' warp lives (its own waits are limited, and it always ends)
     bool got = false;
-    for (int i = 0; i < 64 && !got; ++i)
-      for (uint32_t x = 0; x < WAIT_LIMIT && !got; ++x) got = mbar_try_wait(&sh.go, n & 1);
+#pragma unroll 1
+    for (uint32_t i = 0; i < 4 * WAIT_LIMIT && !got; ++i) {
+      got = *const_cast<volatile int*>(&sh.posted) > n;
+      if (!got) __nanosleep(64);
+    }
     if (!__all_sync(0xffffffffu, got)) {
       atomicOr(p.status + ST_ERR, ERR_TIMEOUT);
       return;
     }
-    const TreeClearJob j = sh.job;
-    if (j.quit) return;
-    const uint32_t tile = ring + j.slot * Z::OPER;
+    __threadfence_block();
+    const TreeClearJob j = sh.jobs[n % TA_JOBS];
+    if (j.slot < 0) return;
+    __all_sync(0xffffffffu, mbar_wait(&sh.v_full[j.slot], j.phase, p.status));
+    const uint32_t tile = v_ring + j.slot * Z::OPER;
+    uint32_t lo = 0, hi = 0;
 #pragma unroll 1
-    for (int r = tid; r < TA_TILE; r += 64) {
+    for (int r = lane; r < TA_TILE; r += 32) {
       const int tok = j.base + r;
-      bool drop = tok >= j.T || !((j.pages >> (r / PAGE)) & 1);
+      bool drop = tok >= j.T;
       if (!drop && tok >= j.C) {
+#pragma unroll 4
         for (int c = 0; c < HD / 8; ++c) {
           const uint4 v = lds128(ta_piece(tile, r, c));
           const uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
           for (int e = 0; e < 4; ++e) drop = drop || (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
         }
-        if (drop)
-          for (int w = 0; w < 2; ++w)
-            if ((j.units >> w) & 1) atomicOr(&sh.dirty[w], 1ull << (tok - j.C));
+        if (drop) {
+          if (tok - j.C < 32) lo |= 1u << (tok - j.C);
+          else hi |= 1u << (tok - j.C - 32);
+        }
       }
       if (drop)
         for (int c = 0; c < HD / 8; ++c)
           asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ta_piece(tile, r, c)), "r"(0u) : "memory");
     }
+    lo = __reduce_or_sync(0xffffffffu, lo);
+    hi = __reduce_or_sync(0xffffffffu, hi);
+    if (lane == 0) sh.dirty[n % TA_JOBS] = (uint64_t)lo | ((uint64_t)hi << 32);
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    mbar_arrive(&sh.clean);
+    mbar_arrive(&sh.v_clean[j.slot]);
   }
 }
 
-// ---- softmax, a row per thread ----
+// ---- tensor cores ----
+// This warp's pace is the kernel's.  It waits for all that a turn needs at once, a barrier per lane, and issues a turn's products
+// and commits in one elected block on operands that are the same in all lanes: 32 to 62 cycles a product, where predicated ones
+// took 80 and blocks on lanes' own values more than that.
+template <int HD>
+__device__ void tree_mma(const TreeDev& p, TreeShared<HD>& sh, uint32_t q_oper, uint32_t k_ring, uint32_t v_ring, int u0, int u1) {
+  using Z = TaSize<HD>;
+  constexpr uint32_t S_IDESC = umma_idesc_bf16_m128(TA_TILE, 0, 0), O_IDESC = umma_idesc_bf16_m128(HD, 0, 1);
+  const int lane = threadIdx.x & 31;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
+  const uint64_t q_desc = umma_smem_desc(q_oper, 16, 1024);
+  const uint64_t k_desc = umma_smem_desc(k_ring, 16, 1024), v_desc = umma_smem_desc(v_ring, Z::CHUNK, 1024);
+  const uint32_t k_full = smem_u32(sh.k_full), v_full = smem_u32(sh.v_full), v_clean = smem_u32(sh.v_clean), p_ready = smem_u32(sh.p_ready);
+  bool alive = true;
+  auto wait = [&](uint32_t bar, uint32_t parity) {  // bar, parity: this lane's.  After one that gave up, the others return at once
+    if (__all_sync(0xffffffffu, mbar_try_wait_at(bar, parity)) || !alive) return;
+    bool ok = false;
+#pragma unroll 1
+    for (uint32_t i = 0; i < WAIT_LIMIT && !ok; ++i) ok = mbar_try_wait_at(bar, parity);
+    alive = __all_sync(0xffffffffu, ok);
+    if (!ok) atomicOr(p.status + ST_ERR, ERR_TIMEOUT);
+  };
+  int k_slot = 0, v_slot = 0;  // of the next tiles
+  uint32_t k_phase = 0, v_phase = 0, clean_phases = 0, p_phases = 0;  // clean_phases, p_phases: a bit per slot, per unit
+  auto k_step = [&]() {
+    if (++k_slot == Z::K_SLOTS) {
+      k_slot = 0;
+      k_phase ^= 1;
+    }
+  };
+  auto v_step = [&]() {
+    if (++v_slot == Z::V_SLOTS) {
+      v_slot = 0;
+      v_phase ^= 1;
+    }
+  };
+  // by the elected lane: a tile's scores, over the unit's last weights, whose product was asked for before
+  auto scores = [&](int unit, uint64_t queries, bool last) {
+    const uint64_t keys = k_desc + (uint64_t)(k_slot * (Z::OPER >> 4));
+#pragma unroll
+    for (int k = 0; k < HD / 16; ++k) {
+      const uint64_t off = ((k >> 2) * Z::CHUNK + (k & 3) * 32) >> 4;
+      umma_bf16(tmem + unit * Z::UNIT, queries + off, keys + off, S_IDESC, k > 0);
+    }
+    umma_commit(&sh.s_full[unit]);
+    if (last) umma_commit(&sh.k_empty[k_slot]);
+  };
+  // ... and the product of the unit's weights with the values
+  auto values = [&](int unit, bool fresh, bool last, bool end) {
+    const uint32_t base = tmem + unit * Z::UNIT;
+    const uint64_t b = v_desc + (uint64_t)(v_slot * (Z::OPER >> 4));
+#pragma unroll
+    for (int k = 0; k < TA_TILE / 16; ++k)
+      umma_bf16_ts(base + TA_TILE, base + k * 8, b + (uint64_t)(k * 2048 >> 4), O_IDESC, !fresh || k > 0);
+    if (last) umma_commit(&sh.v_empty[v_slot]);
+    if (end) {
+      umma_commit(&sh.o_end[unit]);
+      mbar_arrive(&sh.o_end[unit]);  // what this warp has seen, the unit sees: the clearing warp's finds among it
+    }
+  };
+  uint32_t piece = 0;
+  for (int u = u0; u < u1; ++piece) {
+    const TreePiece c = tree_piece(p.c, sh.plan, u, u1);
+    const int steps = c.steps, mixed = c.first_mixed() - c.tile0;
+    wait(smem_u32(&sh.q_ready), piece & 1);
+    // a turn's barriers: the unit's weights, the next keys, the values (cleared, where that is needed)
+    auto turn = [&](int unit, int j, bool keys) {
+      const bool mix = j >= mixed;
+      const uint32_t bar = lane == 0 ? p_ready + unit * 8 : lane == 1 && keys ? k_full + k_slot * 8 : (mix ? v_clean : v_full) + v_slot * 8;
+      const uint32_t parity = lane == 0 ? (p_phases >> unit) & 1 : lane == 1 && keys ? k_phase : mix ? (clean_phases >> v_slot) & 1 : v_phase;
+      wait(bar, parity);
+      p_phases ^= 1u << unit;
+      tc_fence_after();
+    };
+    auto values_used = [&](int j) {
+      if (j >= mixed) clean_phases ^= 1u << v_slot;
+      v_step();
+    };
+    if (c.both) {
+      const uint64_t q1_desc = q_desc + (uint64_t)(Z::OPER >> 4);
+      wait(k_full + k_slot * 8, k_phase);
+      tc_fence_after();
+      if (elect_one()) {
+        scores(0, q_desc, false);
+        scores(1, q1_desc, true);
+      }
+      __syncwarp();
+      k_step();
+#pragma unroll 1
+      for (int j = 0; j < steps; ++j) {
+        const bool more = j + 1 < steps;
+        turn(0, j, more);
+        if (elect_one()) {
+          values(0, j == 0, false, !more);
+          if (more) scores(0, q_desc, false);
+        }
+        __syncwarp();
+        wait(p_ready + 8, (p_phases >> 1) & 1);
+        p_phases ^= 2u;
+        tc_fence_after();
+        if (elect_one()) {
+          values(1, j == 0, true, !more);
+          if (more) scores(1, q1_desc, true);
+        }
+        __syncwarp();
+        values_used(j);
+        if (more) k_step();
+      }
+    } else {
+      for (int j = 0; j < min(2, steps); ++j) {
+        wait(k_full + k_slot * 8, k_phase);
+        tc_fence_after();
+        if (elect_one()) scores(j, q_desc, true);
+        __syncwarp();
+        k_step();
+      }
+#pragma unroll 1
+      for (int j = 0; j < steps; ++j) {
+        const int unit = j & 1;
+        const bool more = j + 2 < steps;
+        turn(unit, j, more);
+        if (elect_one()) {
+          values(unit, j < 2, true, !more);
+          if (more) scores(unit, q_desc, true);
+        }
+        __syncwarp();
+        values_used(j);
+        if (more) k_step();
+      }
+    }
+    u += steps;
+  }
+}
+
+// ---- softmax, a lane per thread ----
 __device__ __forceinline__ void tree_units_sync() {
   __syncwarp();
   asm volatile("bar.sync 1, 256;" ::: "memory");
@@ -330,237 +403,288 @@ __device__ __forceinline__ uint32_t tree_seen(int base, int C, uint64_t nodes) {
   return -ctx < 64 ? (uint32_t)(nodes >> -ctx) : 0u;
 }
 
+// A unit's sums times f, seldom.
+template <int HD>
+__device__ __noinline__ void tree_rescale(uint32_t tm_o, float f) {
+#pragma unroll 1
+  for (int x = 0; x < HD; x += 16) {
+    uint32_t o[16];
+    tmem_ld16_issue(tm_o + x, o);
+    tmem_ld16_wait(o);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+    tmem_st16(tm_o + x, o);
+  }
+}
+
+// A tile's W tokens from column `seg` W of the scores on: weights to the front of the scores' columns (the other tokens' are zero).
+// base: the first of these tokens; m, l: running maximum (base 2) and sum; fresh: the unit has no sums yet.  (Its products so far
+// are over: these scores were asked for after them.)
+template <int HD, int W>
+__device__ __forceinline__ void tree_step(const TreeDev& p, uint32_t tm_s, int seg, int base, int C, uint64_t nodes, int there,
+                                          bool fresh, float& m, float& l) {
+  uint32_t s[W];
+#pragma unroll
+  for (int x = 0; x < W; x += 32) tmem_ld32_issue(tm_s + seg * W + x, s + x);
+#pragma unroll
+  for (int x = 0; x < W; x += 32) tmem_ld32_wait(s + x);
+  if (base + W > C || there != 3) {
+#pragma unroll
+    for (int x = 0; x < W; x += 32) {
+      const uint32_t seen = (there >> ((base + x) / PAGE & 1)) & 1 ? tree_seen(base + x, C, nodes) : 0u;
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (!((seen >> i) & 1)) s[x + i] = 0xff800000u;  // minus infinity
+    }
+  }
+  float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+  for (int i = 0; i < W; i += 2) mx[(i >> 1) & 3] = ta_max3(mx[(i >> 1) & 3], __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+  const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
+  if (__any_sync(0xffffffffu, top > m + TA_SLACK)) {
+    const float m_new = fmaxf(m, top), f = m_new == -INFINITY ? 1.f : ta_exp2(m - m_new);
+    m = m_new;
+    l *= f;
+    if (!fresh) tree_rescale<HD>(tm_s + TA_TILE, f);
+  }
+  const float shift = m == -INFINITY ? 0.f : -m;
+  const uint64_t scale2 = f32x2(p.scale_log2, p.scale_log2), shift2 = f32x2(shift, shift);
+  uint64_t sum[2] = {0, 0};
+  uint32_t w[W / 2];
+#pragma unroll
+  for (int i = 0; i < W / 2; ++i) {
+    const float2 e = ta_unpack2(fma_f32x2(f32x2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), scale2, shift2));
+    const float a = ta_exp2(e.x), b = ta_exp2(e.y);
+    sum[i & 1] = ta_add2(sum[i & 1], f32x2(a, b));
+    w[i] = ta_pack(a, b);
+    if (W == TA_TILE && i == 31) tmem_st32(tm_s, w);
+  }
+  if constexpr (W == TA_TILE) {
+    tmem_st32(tm_s + 32, w + 32);
+  } else {  // seg W / 2 words of zeros, the weights, zeros
+    uint32_t z[32];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) z[i] = seg == (half * 32 + i) / (W / 2) ? w[i % (W / 2)] : 0u;
+      tmem_st32(tm_s + half * 32, z);
+    }
+  }
+  const float2 both = ta_unpack2(ta_add2(sum[0], sum[1]));
+  l += both.x + both.y;
+  tmem_st_wait();
+}
+
+// Drafted tokens whose values were taken out, for a row that sees them: this lane's share of the tokens, columns x .. x + 31.  Rare:
+// kept out of the way of the code that always runs.
+template <int HD>
+__device__ __noinline__ void tree_add_dirty(const TreeDev& p, int b, int kvh, int C, int lanes, uint64_t left, int seg, size_t q_at,
+                                            float m, float f, int x, float* ex, int me) {
+  const uint16_t* q = p.q + q_at;
+  for (; left; left &= left - 1) {
+    const int slot = C + __ffsll((long long)left) - 1;
+    if (slot % TA_TILE / lanes != seg) continue;
+    const int id = p.c.kv.page_table[(size_t)b * p.c.kv.max_pages_per_seq + slot / PAGE];
+    const size_t row = (((size_t)id * p.c.Hkv + kvh) * PAGE + slot % PAGE) * HD;
+    const uint16_t *k = static_cast<const uint16_t*>(p.c.kv.k_pool) + row, *v = static_cast<const uint16_t*>(p.c.kv.v_pool) + row + x;
+    float dot = 0.f;
+    for (int d = 0; d < HD; ++d) dot += bf2f(q[d]) * bf2f(k[d]);
+    const float w = ta_exp2(fmaf(dot, p.scale_log2, m == -INFINITY ? 0.f : -m)) * f;
+    for (int i = 0; i < TA_EX; ++i) ex[i * 256 + (me ^ (i >> 3 << 3))] += w * bf2f(v[i]);
+  }
+}
+
 template <int HD>
 __device__ void tree_softmax(const TreeDev& p, TreeShared<HD>& sh, unsigned char* q_smem, int u0, int u1) {
   using Z = TaSize<HD>;
-  constexpr int EX = HD / 2;  // columns that unit 1 hands over at a time
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, unit = warp >> 2, quad = warp & 3, row_in_unit = quad * 32 + lane;
-  const int G = p.c.G;
-  const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-  const uint32_t tm_s = sh.tmem + unit * Z::UNIT + lanes, tm_o = tm_s + TA_TILE;
-  float* ex = reinterpret_cast<float*>(q_smem + Z::OPER);       // [EX][128] sums of unit 1
-  float2* ex_ml = reinterpret_cast<float2*>(q_smem);            // [2][128], once the scores are done
+  constexpr int PPR = HD / 8, STEP = 256 / PPR;  // 16-byte pieces of a row; rows that 256 threads bring at once
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, unit = warp >> 2, quad = warp & 3, at = quad * 32 + lane;
+  const int G = p.c.G, g_inv = 65536 / G + 1;  // r * g_inv >> 16 is r / G, exact for rows below 512 and groups up to 8
+  const uint32_t tm_s = sh.tmem + unit * Z::UNIT + ((uint32_t)(quad * 32) << 16), tm_o = tm_s + TA_TILE;
+  float* ex = reinterpret_cast<float*>(q_smem + Z::EX);      // [TA_EX][256]: columns of both units' lanes
+  float2* ex_ml = reinterpret_cast<float2*>(q_smem + Z::ML);  // [256]
   bool alive = true;
-  auto wait = [&](uint64_t* bar, uint32_t parity) {  // after one that gave up, the others return at once
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
     alive = alive && mbar_wait(bar, parity, p.status);
     __syncwarp();
   };
-  int done = 0, ends = 0;
-  for (int u = u0; u < u1;) {
-    const TreePiece c = tree_piece(p.c, sh.plan, u, u1);
-    const int T = c.seq.T, n = c.seq.n;
-    tree_units_sync();  // both units are done with the queries of the piece before, and with what lay in their place
-    if ((threadIdx.x & 127) == 0) sh.dirty[unit] = 0;
-    // ---- queries into their operand tiles ----
-    const int block0 = c.block * TA_BLOCK, my_row = (c.both ? unit * TA_ROWS : 0) + row_in_unit;
-    const bool real = my_row < c.rows;
+  // element of q and of the output where row r of the piece's sequence begins
+  auto q_at = [&](const TreePiece& c, int r) {
+    const int node = (r * g_inv) >> 16;
+    return (((size_t)c.b * p.c.max_nodes + node) * p.Hq + c.kvh * G + (r - node * G)) * HD;
+  };
+  auto row_of = [&](const TreePiece& c) { return (c.both ? unit * TA_ROWS : 0) + (at & (c.lanes - 1)); };  // this lane's, of the block
+  if (u0 >= u1) return;
+  TreePiece c = tree_piece(p.c, sh.plan, u0, u1);
+  uint32_t done = 0, ends = 0, jobs = 0;  // tiles weighed, pieces ended, tiles that were cleared
+#pragma unroll 1
+  for (int u = u0;;) {
+    // ---- the queries into their operand tiles, every row once, with its copies; lanes beyond the rows hold zeros ----
     {
-      // a 16-lane (HD 128) or 8-lane group per row; where both units share their rows, each brings half of them
-      constexpr int PPR = HD / 8;
-      const int t = threadIdx.x & 127, per = c.both ? TA_ROWS : TA_ROWS / 2, r0 = c.both ? 0 : unit * per;
-      const uint32_t oper = smem_u32(q_smem) + (c.both ? unit * Z::OPER : 0);
-#pragma unroll 4
-      for (int i = t; i < per * PPR; i += 128) {
-        const int r = r0 + i / PPR, piece = i % PPR, row = block0 + (c.both ? unit * TA_ROWS : 0) + r, node = row / G;
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (row < block0 + c.rows)
-          v = *reinterpret_cast<const uint4*>(
-              p.q + (((size_t)c.b * p.c.max_nodes + node) * p.Hq + c.kvh * G + (row - node * G)) * HD + piece * 8);
-        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(ta_piece(oper, r, piece)), "r"(v.x), "r"(v.y), "r"(v.z),
-                     "r"(v.w)
-                     : "memory");
+      const int rows = c.both ? TA_BLOCK : c.lanes;
+#pragma unroll 1
+      for (int r0 = tid / PPR; r0 < rows; r0 += 4 * STEP) {
+        uint4 q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = r0 + i * STEP;
+          q[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (r < c.rows) q[i] = *reinterpret_cast<const uint4*>(p.q + q_at(c, c.block * TA_BLOCK + r) + tid % PPR * 8);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = r0 + i * STEP;
+          const uint32_t dst = smem_u32(q_smem) + (r >= TA_ROWS ? Z::OPER : 0);
+          if (r >= rows) break;
+#pragma unroll 1
+          for (int to = r & (TA_ROWS - 1); to < TA_ROWS; to += c.lanes)
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(ta_piece(dst, to, tid % PPR)), "r"(q[i].x), "r"(q[i].y),
+                         "r"(q[i].z), "r"(q[i].w)
+                         : "memory");
+        }
       }
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     tc_fence_before();
-    mbar_arrive(&sh.q_ready[unit]);
-    const int node = (block0 + my_row) / G;
+    mbar_arrive(&sh.q_ready);
+    const int block0 = c.block * TA_BLOCK, my_row = row_of(c), seg = at / c.lanes;
+    const bool real = my_row < c.rows, warp_real = my_row - lane < c.rows;
     uint64_t nodes = 0;
-    if (real) nodes = p.mask[(size_t)c.b * p.c.max_nodes + node] & (n < 64 ? (1ull << n) - 1 : ~0ull);
-    const size_t base_row = (((size_t)c.b * p.c.max_nodes + node) * p.Hq + c.kvh * G + (block0 + my_row - node * G)) * HD;
-    const bool warp_real = (c.both ? unit * TA_ROWS : 0) + quad * 32 < c.rows;
-
-    const int32_t* table = p.c.kv.page_table + (size_t)c.b * p.c.kv.max_pages_per_seq;
-    const int pages = (T + PAGE - 1) / PAGE, stride = c.both ? 1 : 2, from = c.both ? 0 : unit;
-    auto page_bits = [&](int step) {
-      int bits = 0;
-      for (int x = 0; x < 2; ++x) {
-        const int i = 2 * (c.tile0 + step) + x;
-        if (step < c.steps && i < pages) {
-          const int id = table[i];
-          bits |= (id >= 0 && id < p.c.kv.num_pages) << x;
-        }
-      }
-      return bits;
+    if (real)
+      nodes = p.mask[(size_t)c.b * p.c.max_nodes + (((block0 + my_row) * g_inv) >> 16)] & (c.seq.n < 64 ? (1ull << c.seq.n) - 1 : ~0ull);
+    const int stride = c.both ? 1 : 2, from = c.both ? 0 : unit, pages = (c.seq.T + PAGE - 1) / PAGE - 2 * c.tile0;
+    const int32_t* table = p.c.kv.page_table + (size_t)c.b * p.c.kv.max_pages_per_seq + 2 * c.tile0;
+    int id0 = -1, id1 = -1;  // pages of the tile to come
+    auto look = [&](int j) {
+      id0 = j < c.steps ? table[2 * j] : -1;
+      id1 = j < c.steps && 2 * j + 1 < pages ? table[2 * j + 1] : 0;
     };
+    look(from);
     float m = -INFINITY, l = 0.f;
-    int there = page_bits(from);
 #pragma unroll 1
-    for (int j = from; j < c.steps; j += stride) {
-      const int base = (c.tile0 + j) * TA_TILE, there_next = page_bits(j + stride);
+    for (int j = from; j < c.steps; j += stride, ++done) {
+      const int base = (c.tile0 + j) * TA_TILE;
+      const int there = (int)(id0 >= 0 && id0 < p.c.kv.num_pages) | (int)(id1 >= 0 && id1 < p.c.kv.num_pages) << 1;
+      look(j + stride);
       wait(&sh.s_full[unit], done & 1);
-      ++done;
       tc_fence_after();
       if (warp_real) {
-        uint32_t s[TA_TILE];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) tmem_ld32_issue(tm_s + x * 32, s + x * 32);
-#pragma unroll
-        for (int x = 0; x < 4; ++x) tmem_ld32_wait(s + x * 32);
-        if (base + TA_TILE > c.C || there != 3) {
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const uint32_t seen = (there >> (x >> 1)) & 1 ? tree_seen(base + 32 * x, c.C, nodes) : 0u;
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (!((seen >> i) & 1)) s[x * 32 + i] = 0xff800000u;  // minus infinity
-          }
-        }
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int i = 0; i < TA_TILE; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(s[i]));
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
-        if (__any_sync(0xffffffffu, top > m + TA_SLACK)) {
-          const float m_new = fmaxf(m, top), f = m_new == -INFINITY ? 1.f : ta_exp2(m - m_new);
-          m = m_new;
-          l *= f;
-          if (j != from) {  // this unit's products so far were done before these scores
-#pragma unroll 1
-            for (int x = 0; x < HD / 32; ++x) {
-              uint32_t o[32];
-              tmem_ld32_issue(tm_o + x * 32, o);
-              tmem_ld32_wait(o);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-              tmem_st32(tm_o + x * 32, o);
-            }
-          }
-        }
-        const float shift = m == -INFINITY ? 0.f : -m;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          uint32_t w[32];
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const float a = ta_exp2(fmaf(__uint_as_float(s[x * 64 + 2 * i]), p.scale_log2, shift));
-            const float b = ta_exp2(fmaf(__uint_as_float(s[x * 64 + 2 * i + 1]), p.scale_log2, shift));
-            sum[(2 * i) & 3] += a;
-            sum[(2 * i + 1) & 3] += b;
-            w[i] = pack_bf16(a, b);
-          }
-          tmem_st32(tm_s + x * 32, w);
-        }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        tmem_st_wait();
+        if (c.lanes == 128) tree_step<HD, 128>(p, tm_s, 0, base, c.C, nodes, there, j == from, m, l);
+        else if (c.lanes == 64) tree_step<HD, 64>(p, tm_s, seg, base + seg * 64, c.C, nodes, there, j == from, m, l);
+        else tree_step<HD, 32>(p, tm_s, seg, base + seg * 32, c.C, nodes, there, j == from, m, l);
       }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.p_ready[unit]);
-      there = there_next;
+    }
+    const int u_next = u + c.steps;
+    TreePiece next = c;
+    if (u_next < u1) {  // the next queries on their way to L2 while this piece ends
+      next = tree_piece(p.c, sh.plan, u_next, u1);
+      for (int r = tid; r < next.rows; r += 256)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(p.q + q_at(next, next.block * TA_BLOCK + r)));
     }
 
-    // ---- the end of the piece ----
-    const bool worked = from < c.steps, pair = !c.both && c.steps > 1;
+    // ---- the end of the piece: what the units, and the copies of a row, have is added up ----
+    const bool worked = from < c.steps, whole = c.whole();
     if (worked) {
-      wait(&sh.o_done[unit], ends & 1);
+      wait(&sh.o_end[unit], ends & 1);
       ++ends;
     }
     tc_fence_after();
-    const uint64_t dirty = worked && real && c.tile1 * TA_TILE > c.C ? sh.dirty[unit] & nodes : 0ull;
-    float f = 1.f;
-    if (pair) {  // both units' rows are the same: with the larger maximum from here on
-      ex_ml[unit * 128 + row_in_unit] = make_float2(m, l);
-      tree_units_sync();
-      const float2 other = ex_ml[(unit ^ 1) * 128 + row_in_unit];
-      const float m_new = fmaxf(m, other.x);
-      f = m_new == -INFINITY ? 1.f : exp2f(m - m_new);
-      l = l * f + other.y * (m_new == -INFINITY ? 1.f : exp2f(other.x - m_new));
-      if (dirty == 0) m = m_new;
-    }
-    const float m_own = m;  // what this unit's sums are relative to, where dirty tokens are added
-    if (pair && dirty) m = fmaxf(m, ex_ml[(unit ^ 1) * 128 + row_in_unit].x);
-    const bool whole = c.whole(), writes = real && (c.both || unit == 0);
-    const float inv = whole ? (l == 0.f ? 0.f : 1.0f / l) : 1.f;
-    const size_t part = (size_t)(2 * blockIdx.x + (u > u0)) * p.part.rows + my_row;
+    tree_units_sync();  // nobody reads the queries any more
+    const int pad = c.both ? 256 : c.lanes, me = unit * 128 + at;
+    const size_t part = (size_t)(2 * blockIdx.x + (u > u0)) * p.part.rows;
+    ex_ml[me] = make_float2(m, l);
+    tree_units_sync();
+    float top = -INFINITY, sum = 0.f;
 #pragma unroll 1
-    for (int x = 0; x < HD / 32; ++x) {
-      uint32_t o[32];
-      float v[32];
-      __syncwarp();
+    for (int i = me & (pad - 1); i < 256; i += pad) top = fmaxf(top, ex_ml[i].x);
+    const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll 1
+    for (int i = me & (pad - 1); i < 256; i += pad) {
+      const float2 v = ex_ml[i];
+      sum += v.y * ta_exp2(v.x - base);
+    }
+    const float f = ta_exp2(m - base);
+    tree_units_sync();
+    if (me < pad) {
+      ex_ml[me] = make_float2(top, sum);
+      if (real && !whole) p.part.ml[part + my_row] = make_float2(top, sum);
+    }
+    uint64_t dirty = 0;  // drafted tokens whose values were taken out, of this unit's tiles
+    for (int t = c.first_mixed(); t < c.tile1; ++t, ++jobs)
+      if (c.both || ((t - c.tile0) & 1) == unit) dirty |= sh.dirty[jobs % TA_JOBS];
+    dirty = worked && real ? dirty & nodes : 0ull;
+    // 32 columns at a time: every lane leaves its own, then a thread adds up eight columns of a row (the places are turned by the
+    // columns' group, so that the four threads of a row read from different banks)
+#pragma unroll 1
+    for (int x = 0; x < HD; x += TA_EX) {
+      uint32_t o[TA_EX];
+#pragma unroll
+      for (int i = 0; i < TA_EX; ++i) o[i] = 0u;
       if (warp_real && worked) {
-        tmem_ld32_issue(tm_o + x * 32, o);
+        tmem_ld32_issue(tm_o + x, o);
         tmem_ld32_wait(o);
       }
 #pragma unroll
-      for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(o[i]);
-      if (dirty) {
-        for (uint64_t left = dirty; left; left &= left - 1) {
-          const int slot = c.C + __ffsll((long long)left) - 1, id = table[slot / PAGE];
-          const size_t at = (((size_t)id * p.c.Hkv + c.kvh) * PAGE + slot % PAGE) * HD;
-          const uint16_t *kr = static_cast<const uint16_t*>(p.c.kv.k_pool) + at, *vr = static_cast<const uint16_t*>(p.c.kv.v_pool) + at;
-          float dot = 0.f;
-          for (int d = 0; d < HD; ++d) dot += bf2f(p.q[base_row + d]) * bf2f(kr[d]);
-          const float w = ta_exp2(fmaf(dot, p.scale_log2, m_own == -INFINITY ? 0.f : -m_own));
+      for (int i = 0; i < TA_EX; ++i) ex[i * 256 + (me ^ (i >> 3 << 3))] = __uint_as_float(o[i]) * f;
+      if (dirty) tree_add_dirty<HD>(p, c.b, c.kvh, c.C, c.lanes, dirty, seg, q_at(c, block0 + my_row), m, f, x, ex, me);
+      tree_units_sync();
+#pragma unroll 1
+      for (int t = threadIdx.x; t < pad * 4; t += 256) {
+        const int r = t >> 2, col = (t & 3) * 8;
+        if (r >= c.rows) break;
+        float a[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+        for (int i = r; i < 256; i += pad)
 #pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] += w * bf2f(vr[x * 32 + i]);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 32; ++i) v[i] *= f;
-      if (pair) {
-        // unit 1's columns 0 .. EX - 1, then the others, by way of shared memory
-        const int half = x * 32 / EX;
-        if (unit == 1)
-#pragma unroll
-          for (int i = 0; i < 32; ++i) ex[(x * 32 - half * EX + i) * 128 + row_in_unit] = v[i];
-        tree_units_sync();
-        if (unit == 0)
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] += ex[(x * 32 - half * EX + i) * 128 + row_in_unit];
-        if ((x + 1) * 32 == EX) tree_units_sync();  // the first half's space is used again
-      }
-      if (writes) {
+          for (int e = 0; e < 8; ++e) a[e] += ex[(col + e) * 256 + (i ^ col)];
         if (whole) {
-          uint4* dst = reinterpret_cast<uint4*>(p.out + base_row + x * 32);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            dst[i] = make_uint4(pack_bf16(v[8 * i] * inv, v[8 * i + 1] * inv), pack_bf16(v[8 * i + 2] * inv, v[8 * i + 3] * inv),
-                                pack_bf16(v[8 * i + 4] * inv, v[8 * i + 5] * inv), pack_bf16(v[8 * i + 6] * inv, v[8 * i + 7] * inv));
+          const float total = ex_ml[r].y, inv = total == 0.f ? 0.f : 1.0f / total;
+          *reinterpret_cast<uint4*>(p.out + q_at(c, block0 + r) + x + col) =
+              make_uint4(ta_pack(a[0] * inv, a[1] * inv), ta_pack(a[2] * inv, a[3] * inv), ta_pack(a[4] * inv, a[5] * inv),
+                         ta_pack(a[6] * inv, a[7] * inv));
         } else {
-          float4* dst = reinterpret_cast<float4*>(p.part.sums + part * HD + x * 32);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) dst[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+          float4* dst = reinterpret_cast<float4*>(p.part.sums + (part + r) * HD + x + col);
+          dst[0] = make_float4(a[0], a[1], a[2], a[3]);
+          dst[1] = make_float4(a[4], a[5], a[6], a[7]);
         }
       }
+      tree_units_sync();
     }
-    if (writes && !whole) p.part.ml[part] = make_float2(m, l);
-    u += c.steps;
+    if (u_next >= u1) break;
+    c = next;
+    u = u_next;
   }
 }
 
 template <int HD>
 __global__ void __launch_bounds__(TA_THREADS, 1) tree_attn_kernel(const __grid_constant__ CUtensorMap kmap,
-                                                                  const __grid_constant__ CUtensorMap vmap, const TreeDev p) {
+                                                                  const __grid_constant__ CUtensorMap vmap, const __grid_constant__ TreeDev p) {
   using Z = TaSize<HD>;
   extern __shared__ unsigned char ta_smem[];
   __shared__ TreeShared<HD> sh;
   unsigned char* q_smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(ta_smem) + 1023) & ~(uintptr_t)1023);
-  unsigned char* ring = q_smem + 2 * Z::OPER;
+  unsigned char *k_ring = q_smem + 2 * Z::OPER, *v_ring = k_ring + Z::K_SLOTS * Z::OPER;
   const int tid = threadIdx.x, warp = tid >> 5;
   if (tid == 0) {
-    for (int s = 0; s < Z::SLOTS; ++s) {
-      mbar_init(&sh.full[s], 1);
-      mbar_init(&sh.empty[s], 1);
+    for (int i = 0; i < Z::K_SLOTS; ++i) {
+      mbar_init(&sh.k_full[i], 1);
+      mbar_init(&sh.k_empty[i], 1);
     }
+    for (int i = 0; i < Z::V_SLOTS; ++i) {
+      mbar_init(&sh.v_full[i], 1);
+      mbar_init(&sh.v_empty[i], 1);
+      mbar_init(&sh.v_clean[i], 32);
+    }
+    mbar_init(&sh.q_ready, 256);
     for (int x = 0; x < 2; ++x) {
-      mbar_init(&sh.q_ready[x], TA_ROWS);
       mbar_init(&sh.s_full[x], 1);
       mbar_init(&sh.p_ready[x], 4);
-      mbar_init(&sh.o_done[x], 2);
+      mbar_init(&sh.o_end[x], 2);
     }
-    mbar_init(&sh.go, 1);
-    mbar_init(&sh.clean, 64);
+    sh.posted = 0;
     fence_mbar_init();
     tma_prefetch_map(&kmap);
     tma_prefetch_map(&vmap);
@@ -573,10 +697,17 @@ __global__ void __launch_bounds__(TA_THREADS, 1) tree_attn_kernel(const __grid_c
   tc_fence_after();
   const int run = chain_run(p.c, sh.plan, gridDim.x), total = sh.plan.cum[p.c.B];
   const int u0 = (int)min((long long)blockIdx.x * run, (long long)total), u1 = min(total, u0 + run);
+  if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");  // 168 a thread at launch: 128 threads give 64 each,
+  else asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");            // 256 take 32 each
   if (warp < 8) tree_softmax<HD>(p, sh, q_smem, u0, u1);
-  else if (warp == TAW_LOAD) tree_load<HD>(p, sh, ring, &kmap, &vmap, u0, u1);
-  else if (warp == TAW_MMA) tree_mma<HD>(p, sh, smem_u32(q_smem), smem_u32(ring), u0, u1);
-  else tree_clear<HD>(p, sh, smem_u32(ring));
+  else if (warp == TAW_KEYS) tree_load<HD, false>(p, sh, k_ring, &kmap, u0, u1);
+  else if (warp == TAW_VALUES) tree_load<HD, true>(p, sh, v_ring, &vmap, u0, u1);
+  else if (warp == TAW_MMA) tree_mma<HD>(p, sh, smem_u32(q_smem), smem_u32(k_ring), smem_u32(v_ring), u0, u1);
+  else {
+    if (tid == TAW_CLEAR * 32) chain_describe(p.c, sh.plan, run, blockIdx.x, u0, u1, p.part.desc);
+    __syncwarp();
+    tree_clear<HD>(p, sh, smem_u32(v_ring));
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == TAW_MMA) tmem_dealloc(sh.tmem, 512);
