@@ -2,10 +2,12 @@
 // attention weights).
 //
 // A chain is what one softmax runs along: a (sequence, kv-head, block of query rows) over the sequence's tokens, a tile of one
-// or two cache pages at a time.  The tiles of all chains, one chain after the other, form one line, and every CTA takes an
-// equal run of it, whatever the lengths are.  A run covers the end of one chain, some whole chains and the beginning of another: results of whole chains
-// go straight to the output, the first and the last piece go to one of the CTA's two slots of partial results, and a second
-// kernel merges the chains that were cut.  Every CTA of either kernel makes the line for itself from the lengths (at most 128).
+// or two cache pages at a time.  The tiles of all chains, one chain after the other, form one line, of which every CTA takes a
+// run.  A run that ends inside a chain leaves a partial result; a second kernel merges the pieces of chains that were cut.
+// Two ways to cut, of which every CTA works out for itself, from the lengths (at most 128), which one is the better:
+//   equal runs       whatever the lengths are.  A run covers the end of one chain, some whole chains and the beginning of another
+//   CTAs per chain   in proportion to its tiles, one at least: every CTA has one piece.  Taken if that costs no more than the
+//                    second piece that equal runs give most CTAs (beginning and ending a piece takes as long as piece_cost tiles)
 #pragma once
 #include "sol_common.cuh"
 #include "sol_internal.h"
@@ -33,13 +35,6 @@ __device__ __forceinline__ ChainSeq chain_seq(const sol_kv_t& kv, const int32_t*
   return s;
 }
 
-// The line of tiles.  cum[b]: tiles of the sequences before b; seq: lengths.
-struct ChainPlan {
-  int cum[CHAIN_MAX_BATCH + 1];
-  ChainSeq seq[CHAIN_MAX_BATCH];
-  int wsum[4];
-};
-
 struct ChainShape {
   sol_kv_t kv;
   int B, Hkv, G, max_nodes;
@@ -47,9 +42,25 @@ struct ChainShape {
   int block_rows;          // query rows of a chain
   int tile;                // tokens of a tile: PAGE or 2 PAGE
   int min_tiles;           // tiles of a CTA's run at least
+  int piece_cost;          // tiles that beginning and ending a piece is worth
 };
 
-inline ChainShape chain_shape(const RowsArgs& a, int block_rows, int tile, int min_tiles) {
+// The line of tiles.
+struct ChainPlan {
+  int cum[CHAIN_MAX_BATCH + 1];    // tiles of the sequences before b
+  int first[CHAIN_MAX_BATCH + 1];  // CTAs per chain: CTAs of the sequences before b
+  uint32_t seq[CHAIN_MAX_BATCH];   // T << 8 | n
+  int wsum[8];
+  int run;                         // equal runs: tiles of each; 0: CTAs per chain
+  __device__ __forceinline__ ChainSeq at(int b) const {
+    ChainSeq s;
+    s.T = (int)(seq[b] >> 8);
+    s.n = (int)(seq[b] & 255u);
+    return s;
+  }
+};
+
+inline ChainShape chain_shape(const RowsArgs& a, int block_rows, int tile, int min_tiles, int piece_cost) {
   ChainShape c;
   c.kv = a.kv;
   c.B = a.B;
@@ -60,6 +71,7 @@ inline ChainShape chain_shape(const RowsArgs& a, int block_rows, int tile, int m
   c.block_rows = block_rows;
   c.tile = tile;
   c.min_tiles = min_tiles;
+  c.piece_cost = piece_cost;
   return c;
 }
 
@@ -68,37 +80,39 @@ __device__ __forceinline__ int chain_tiles(const ChainShape& c, const ChainSeq& 
 }
 __device__ __forceinline__ int chain_blocks(const ChainShape& c, const ChainSeq& s) { return (s.n * c.G + c.block_rows - 1) / c.block_rows; }
 
-// By the whole CTA (128 threads at least); ends with a barrier.
-__device__ __forceinline__ void chain_plan(const ChainShape& c, ChainPlan& p, int* status) {
+// For a kernel of `ctas` CTAs, by a whole CTA (128 threads at least); ends with a barrier.
+__device__ __forceinline__ void chain_plan(const ChainShape& c, ChainPlan& p, int ctas, int* status) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  int tiles = 0;
-  if (tid < CHAIN_MAX_BATCH) {
-    ChainSeq s;
-    s.T = s.n = 0;
-    if (tid < c.B) {
-      s = chain_seq(c.kv, c.n_nodes, c.max_nodes, tid, status);
-      tiles = s.n > 0 ? chain_tiles(c, s) * chain_blocks(c, s) * c.Hkv : 0;
-    }
-    p.seq[tid] = s;
+  auto scan = [&](int v, int* out) {  // out[b + 1] = v of sequences 0 .. b
+    if (tid < CHAIN_MAX_BATCH) {
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, tiles, o);
-      if (lane >= o) tiles += x;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += x;
+      }
+      if (lane == 31) p.wsum[warp] = v;
     }
-    if (lane == 31) p.wsum[warp] = tiles;
-  }
+    __syncthreads();
+    if (tid < CHAIN_MAX_BATCH) {
+      for (int w = 0; w < warp; ++w) v += p.wsum[w];
+      out[tid + 1] = v;
+      if (tid == 0) out[0] = 0;
+    }
+    __syncthreads();
+  };
+  ChainSeq s;
+  s.T = s.n = 0;
+  if (tid < c.B) s = chain_seq(c.kv, c.n_nodes, c.max_nodes, tid, status);
+  if (tid < CHAIN_MAX_BATCH) p.seq[tid] = (uint32_t)s.T << 8 | (uint32_t)s.n;
+  const int chains = s.n > 0 ? chain_blocks(c, s) * c.Hkv : 0, tiles = chain_tiles(c, s);
+  scan(tiles * chains, p.cum);
+  const int total = p.cum[c.B], run = max(c.min_tiles, (total + ctas - 1) / ctas);
+  const int share = max(1, (int)((long long)tiles * ctas / max(total, 1)));  // CTAs of each of the sequence's chains
+  const int give = min(share, max(1, tiles / c.min_tiles));
+  scan(give * chains, p.first);
+  const int worst = __syncthreads_or(chains > 0 && (tiles + give - 1) / give > run + c.piece_cost);
+  if (tid == 0) p.run = worst || p.first[c.B] > ctas ? run : 0;
   __syncthreads();
-  if (tid < CHAIN_MAX_BATCH) {
-    for (int w = 0; w < warp; ++w) tiles += p.wsum[w];
-    p.cum[tid + 1] = tiles;
-    if (tid == 0) p.cum[0] = 0;
-  }
-  __syncthreads();
-}
-
-// Tiles of a CTA's run, for `ctas` CTAs.
-__device__ __forceinline__ int chain_run(const ChainShape& c, const ChainPlan& p, int ctas) {
-  return max(c.min_tiles, (p.cum[c.B] + ctas - 1) / ctas);
 }
 
 // The sequence that holds tile u of the line.
@@ -112,6 +126,26 @@ __device__ __forceinline__ int chain_find(const ChainShape& c, const ChainPlan& 
   return lo;
 }
 
+// The run of tiles [u0, u1) of a CTA.
+__device__ __forceinline__ int2 chain_range(const ChainShape& c, const ChainPlan& p, int cta) {
+  const int total = p.cum[c.B];
+  if (p.run) {
+    const int u0 = (int)min((long long)cta * p.run, (long long)total);
+    return make_int2(u0, min(total, u0 + p.run));
+  }
+  if (cta >= p.first[c.B]) return make_int2(total, total);
+  int lo = 0, hi = c.B - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (p.first[mid] <= cta) lo = mid;
+    else hi = mid - 1;
+  }
+  const ChainSeq s = p.at(lo);
+  const int tiles = chain_tiles(c, s), each = (p.first[lo + 1] - p.first[lo]) / (chain_blocks(c, s) * c.Hkv);
+  const int local = cta - p.first[lo], chain = local / each, i = local - chain * each, base = p.cum[lo] + chain * tiles;
+  return make_int2(base + (int)((long long)tiles * i / each), base + (int)((long long)tiles * (i + 1) / each));
+}
+
 // A run's next piece: tiles [tile0, tile1) of a chain.
 struct ChainPiece {
   int b, kvh, block;
@@ -122,7 +156,7 @@ struct ChainPiece {
 __device__ __forceinline__ ChainPiece chain_piece(const ChainShape& c, const ChainPlan& p, int u, int end) {
   ChainPiece r;
   r.b = chain_find(c, p, u);
-  r.seq = p.seq[r.b];
+  r.seq = p.at(r.b);
   r.tiles = chain_tiles(c, r.seq);
   const int local = u - p.cum[r.b], chain = local / r.tiles, blocks = chain_blocks(c, r.seq);
   r.tile0 = local - chain * r.tiles;
@@ -140,12 +174,20 @@ struct ChainCut {
   __device__ __forceinline__ int slot(int i) const { return i == 0 ? first_slot : 2 * (first + i); }  // of piece i
   __device__ __forceinline__ int pieces() const { return last - first + 1; }
 };
-__device__ __forceinline__ ChainCut chain_cut(const ChainShape& c, const ChainPlan& p, int run, int b, int chain) {
-  const int tiles = chain_tiles(c, p.seq[b]), u0 = p.cum[b] + chain * tiles;
+__device__ __forceinline__ ChainCut chain_cut(const ChainShape& c, const ChainPlan& p, int b, int chain) {
+  const ChainSeq s = p.at(b);
   ChainCut r;
-  r.first = u0 / run;
-  r.last = (u0 + tiles - 1) / run;
-  r.first_slot = 2 * r.first + (u0 % run ? 1 : 0);
+  if (p.run) {
+    const int tiles = chain_tiles(c, s), u0 = p.cum[b] + chain * tiles;
+    r.first = u0 / p.run;
+    r.last = (u0 + tiles - 1) / p.run;
+    r.first_slot = 2 * r.first + (u0 % p.run ? 1 : 0);
+  } else {
+    const int each = (p.first[b + 1] - p.first[b]) / (chain_blocks(c, s) * c.Hkv);
+    r.first = p.first[b] + chain * each;
+    r.last = r.first + each - 1;
+    r.first_slot = 2 * r.first;
+  }
   return r;
 }
 
@@ -175,19 +217,20 @@ inline ChainParts chain_parts(void* base, int ctas, int rows, int hd) {
 }
 
 // What CTA `cta` with run [u0, u1) of the line leaves to be merged, by one thread.
-__device__ __forceinline__ void chain_describe(const ChainShape& c, const ChainPlan& p, int run, int cta, int u0, int u1, ChainDesc* out) {
+__device__ __forceinline__ void chain_describe(const ChainShape& c, const ChainPlan& p, int cta, int u0, int u1, ChainDesc* out) {
   ChainDesc d;
   d.pieces = d.b = d.kvh = d.block = d.rows = d.first_slot = 0;
   if (u0 < u1) {
     const ChainPiece last = chain_piece(c, p, u1 - 1, u1);
     const int start = u1 - 1 - last.tile0;
     if (last.tile0 + 1 < last.tiles && start >= u0) {
-      d.pieces = (start + last.tiles - 1) / run - cta + 1;
+      const ChainCut cut = chain_cut(c, p, last.b, last.kvh * chain_blocks(c, last.seq) + last.block);
+      d.pieces = cut.pieces();
+      d.first_slot = cut.first_slot;
       d.b = last.b;
       d.kvh = last.kvh;
       d.block = last.block;
       d.rows = min(c.block_rows, last.seq.n * c.G - last.block * c.block_rows);
-      d.first_slot = 2 * cta + (start > u0);
     }
   }
   out[cta] = d;

@@ -26,6 +26,7 @@ constexpr int RA_WARPS = 6;   // consumer warps
 constexpr int RA_DEPTH = 2;   // stages of a warp's ring
 constexpr int RA_THREADS = (RA_WARPS + 1) * 32;
 constexpr int RA_MIN_TILES = 4;
+constexpr int RA_PIECE_COST = 8;
 
 struct RowsDev {
   ChainShape c;
@@ -86,11 +87,11 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
   }
   pdl_wait();
   pdl_trigger();
-  chain_plan(p.c, plan, blockIdx.x == 0 ? p.status : nullptr);
-  const int run = chain_run(p.c, plan, gridDim.x);
-  const int u0 = (int)min((long long)blockIdx.x * run, (long long)plan.cum[p.c.B]), u1 = min(plan.cum[p.c.B], u0 + run);
+  chain_plan(p.c, plan, gridDim.x, blockIdx.x == 0 ? p.status : nullptr);
+  const int2 range = chain_range(p.c, plan, blockIdx.x);
+  const int u0 = range.x, u1 = range.y;
 
-  if (tid == 0) chain_describe(p.c, plan, run, blockIdx.x, u0, u1, p.part.desc);
+  if (tid == 0) chain_describe(p.c, plan, blockIdx.x, u0, u1, p.part.desc);
   if (warp == RA_WARPS) {  // ---- the producer ----
     int it = 0;
     for (int u = u0; u < u1;) {
@@ -428,13 +429,13 @@ __global__ void __launch_bounds__(RM_THREADS) weight_kernel(const RowsDev p, int
   __shared__ int units[CHAIN_MAX_BATCH + 1];
   const int tid = threadIdx.x;
   pdl_trigger();
-  chain_plan(p.c, plan, nullptr);
-  const int run = chain_run(p.c, plan, ctas), G = p.c.G;
+  chain_plan(p.c, plan, ctas, nullptr);
+  const int G = p.c.G;
   if (tid == 0) {
     int n = 0;
     for (int b = 0; b < p.c.B; ++b) {
       units[b] = n;
-      n += max(1, (plan.seq[b].T + WK_TOKENS - 1) / WK_TOKENS) * p.c.Hkv;
+      n += max(1, (plan.at(b).T + WK_TOKENS - 1) / WK_TOKENS) * p.c.Hkv;
     }
     units[p.c.B] = n;
   }
@@ -448,9 +449,9 @@ __global__ void __launch_bounds__(RM_THREADS) weight_kernel(const RowsDev p, int
       if (units[mid] <= u) lo = mid;
       else hi = mid - 1;
     }
-    const int b = lo, T = plan.seq[b].T, per = max(1, (T + WK_TOKENS - 1) / WK_TOKENS);
+    const int b = lo, T = plan.at(b).T, per = max(1, (T + WK_TOKENS - 1) / WK_TOKENS);
     const int kvh = (u - units[b]) / per, chunk = (u - units[b]) - kvh * per;
-    const ChainCut cut = chain_cut(p.c, plan, run, b, kvh);
+    const ChainCut cut = chain_cut(p.c, plan, b, kvh);
     __syncthreads();
     if (cut.cut()) {
       const int g = tid >> 4;
@@ -505,7 +506,7 @@ void launch_rows_attention(const RowsArgs& a, cudaStream_t st) {
     return;
   RowsDev d;
   memset(&d, 0, sizeof(d));
-  d.c = chain_shape(a, RA_ROWS, PAGE, RA_MIN_TILES);
+  d.c = chain_shape(a, RA_ROWS, PAGE, RA_MIN_TILES, RA_PIECE_COST);
   d.Hq = sh.n_q_heads;
   d.scale_log2 = 1.4426950408889634f / sqrtf((float)sh.head_dim);
   d.mask = a.mask;

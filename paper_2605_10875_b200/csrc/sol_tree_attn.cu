@@ -33,6 +33,7 @@ constexpr int TA_ROWS = 128;            // lanes of a unit
 constexpr int TA_BLOCK = 2 * TA_ROWS;   // rows of a chain
 constexpr int TA_TILE = 2 * PAGE;       // tokens of a tile
 constexpr int TA_MIN_TILES = 2;
+constexpr int TA_PIECE_COST = 6;
 constexpr int TA_THREADS = 12 * 32;
 constexpr float TA_SLACK = 8.f;         // weights reach 2^8 before the maximum moves
 constexpr int TA_EX = 32;               // columns handed over at a time at the end of a piece
@@ -519,20 +520,24 @@ __device__ void tree_softmax(const TreeDev& p, TreeShared<HD>& sh, unsigned char
   uint32_t done = 0, ends = 0, jobs = 0;  // tiles weighed, pieces ended, tiles that were cleared
 #pragma unroll 1
   for (int u = u0;;) {
+    const int block0 = c.block * TA_BLOCK, my_row = row_of(c), seg = at / c.lanes;
+    const bool real = my_row < c.rows, warp_real = my_row - lane < c.rows;
+    uint64_t nodes = 0;
+    if (real) nodes = p.mask[(size_t)c.b * p.c.max_nodes + (((block0 + my_row) * g_inv) >> 16)];
     // ---- the queries into their operand tiles, every row once, with its copies; lanes beyond the rows hold zeros ----
     {
       const int rows = c.both ? TA_BLOCK : c.lanes;
 #pragma unroll 1
-      for (int r0 = tid / PPR; r0 < rows; r0 += 4 * STEP) {
-        uint4 q[4];
+      for (int r0 = tid / PPR; r0 < rows; r0 += 8 * STEP) {
+        uint4 q[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 8; ++i) {
           const int r = r0 + i * STEP;
           q[i] = make_uint4(0u, 0u, 0u, 0u);
-          if (r < c.rows) q[i] = *reinterpret_cast<const uint4*>(p.q + q_at(c, c.block * TA_BLOCK + r) + tid % PPR * 8);
+          if (r < c.rows) q[i] = *reinterpret_cast<const uint4*>(p.q + q_at(c, block0 + r) + tid % PPR * 8);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 8; ++i) {
           const int r = r0 + i * STEP;
           const uint32_t dst = smem_u32(q_smem) + (r >= TA_ROWS ? Z::OPER : 0);
           if (r >= rows) break;
@@ -547,25 +552,22 @@ __device__ void tree_softmax(const TreeDev& p, TreeShared<HD>& sh, unsigned char
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     tc_fence_before();
     mbar_arrive(&sh.q_ready);
-    const int block0 = c.block * TA_BLOCK, my_row = row_of(c), seg = at / c.lanes;
-    const bool real = my_row < c.rows, warp_real = my_row - lane < c.rows;
-    uint64_t nodes = 0;
-    if (real)
-      nodes = p.mask[(size_t)c.b * p.c.max_nodes + (((block0 + my_row) * g_inv) >> 16)] & (c.seq.n < 64 ? (1ull << c.seq.n) - 1 : ~0ull);
-    const int stride = c.both ? 1 : 2, from = c.both ? 0 : unit, pages = (c.seq.T + PAGE - 1) / PAGE - 2 * c.tile0;
+    if (c.seq.n < 64) nodes &= (1ull << c.seq.n) - 1;
+    const int stride = c.both ? 1 : 2, from = c.both ? 0 : unit;
     const int32_t* table = p.c.kv.page_table + (size_t)c.b * p.c.kv.max_pages_per_seq + 2 * c.tile0;
-    int id0 = -1, id1 = -1;  // pages of the tile to come
-    auto look = [&](int j) {
-      id0 = j < c.steps ? table[2 * j] : -1;
-      id1 = j < c.steps && 2 * j + 1 < pages ? table[2 * j + 1] : 0;
-    };
-    look(from);
+    const int pages = min((c.seq.T + PAGE - 1) / PAGE - 2 * c.tile0, 2 * c.steps);  // of the piece
+    bool bad = false;
+#pragma unroll 4
+    for (int i = lane; i < pages; i += 32) bad |= (unsigned)table[i] >= (unsigned)p.c.kv.num_pages;
+    bad = __any_sync(0xffffffffu, bad);  // a page is out of range: each tile's pages are looked up
     float m = -INFINITY, l = 0.f;
 #pragma unroll 1
     for (int j = from; j < c.steps; j += stride, ++done) {
       const int base = (c.tile0 + j) * TA_TILE;
-      const int there = (int)(id0 >= 0 && id0 < p.c.kv.num_pages) | (int)(id1 >= 0 && id1 < p.c.kv.num_pages) << 1;
-      look(j + stride);
+      int there = 3;
+      if (bad)
+        there = (int)((unsigned)table[2 * j] < (unsigned)p.c.kv.num_pages) |
+                (int)(2 * j + 1 < pages && (unsigned)table[2 * j + 1] < (unsigned)p.c.kv.num_pages) << 1;
       wait(&sh.s_full[unit], done & 1);
       tc_fence_after();
       if (warp_real) {
@@ -593,24 +595,24 @@ __device__ void tree_softmax(const TreeDev& p, TreeShared<HD>& sh, unsigned char
     }
     tc_fence_after();
     tree_units_sync();  // nobody reads the queries any more
-    const int pad = c.both ? 256 : c.lanes, me = unit * 128 + at;
+    const int pad = c.both ? 256 : c.lanes, me = unit * 128 + at, first = me & (pad - 1);
     const size_t part = (size_t)(2 * blockIdx.x + (u > u0)) * p.part.rows;
     ex_ml[me] = make_float2(m, l);
     tree_units_sync();
-    float top = -INFINITY, sum = 0.f;
-#pragma unroll 1
-    for (int i = me & (pad - 1); i < 256; i += pad) top = fmaxf(top, ex_ml[i].x);
-    const float base = top == -INFINITY ? 0.f : top;
-#pragma unroll 1
-    for (int i = me & (pad - 1); i < 256; i += pad) {
-      const float2 v = ex_ml[i];
-      sum += v.y * ta_exp2(v.x - base);
-    }
-    const float f = ta_exp2(m - base);
-    tree_units_sync();
-    if (me < pad) {
-      ex_ml[me] = make_float2(top, sum);
-      if (real && !whole) p.part.ml[part + my_row] = make_float2(top, sum);
+    float f;  // what this lane's sums count
+    {
+      float2 ml[8];  // a row's shares: one, two, four or eight
+      float top = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ml[i] = first + i * pad < 256 ? ex_ml[first + i * pad] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, ml[i].x);
+      const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += ml[i].y * ta_exp2(ml[i].x - base);
+      f = ta_exp2(m - base);
+      if (whole) f = sum == 0.f ? 0.f : f / sum;
+      else if (me < pad && real) p.part.ml[part + my_row] = make_float2(top, sum);
     }
     uint64_t dirty = 0;  // drafted tokens whose values were taken out, of this unit's tiles
     for (int t = c.first_mixed(); t < c.tile1; ++t, ++jobs)
@@ -632,7 +634,7 @@ __device__ void tree_softmax(const TreeDev& p, TreeShared<HD>& sh, unsigned char
       if (dirty) tree_add_dirty<HD>(p, c.b, c.kvh, c.C, c.lanes, dirty, seg, q_at(c, block0 + my_row), m, f, x, ex, me);
       tree_units_sync();
 #pragma unroll 1
-      for (int t = threadIdx.x; t < pad * 4; t += 256) {
+      for (int t = tid; t < pad * 4; t += 256) {
         const int r = t >> 2, col = (t & 3) * 8;
         if (r >= c.rows) break;
         float a[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -641,10 +643,8 @@ __device__ void tree_softmax(const TreeDev& p, TreeShared<HD>& sh, unsigned char
 #pragma unroll
           for (int e = 0; e < 8; ++e) a[e] += ex[(col + e) * 256 + (i ^ col)];
         if (whole) {
-          const float total = ex_ml[r].y, inv = total == 0.f ? 0.f : 1.0f / total;
           *reinterpret_cast<uint4*>(p.out + q_at(c, block0 + r) + x + col) =
-              make_uint4(ta_pack(a[0] * inv, a[1] * inv), ta_pack(a[2] * inv, a[3] * inv), ta_pack(a[4] * inv, a[5] * inv),
-                         ta_pack(a[6] * inv, a[7] * inv));
+              make_uint4(ta_pack(a[0], a[1]), ta_pack(a[2], a[3]), ta_pack(a[4], a[5]), ta_pack(a[6], a[7]));
         } else {
           float4* dst = reinterpret_cast<float4*>(p.part.sums + (part + r) * HD + x + col);
           dst[0] = make_float4(a[0], a[1], a[2], a[3]);
@@ -693,10 +693,10 @@ __global__ void __launch_bounds__(TA_THREADS, 1) tree_attn_kernel(const __grid_c
   pdl_trigger();
   if (warp == TAW_MMA) tmem_alloc(&sh.tmem, 512);  // not ahead of the wait: a kernel before this one may need it
   tc_fence_before();
-  chain_plan(p.c, sh.plan, blockIdx.x == 0 ? p.status : nullptr);
+  chain_plan(p.c, sh.plan, gridDim.x, blockIdx.x == 0 ? p.status : nullptr);
   tc_fence_after();
-  const int run = chain_run(p.c, sh.plan, gridDim.x), total = sh.plan.cum[p.c.B];
-  const int u0 = (int)min((long long)blockIdx.x * run, (long long)total), u1 = min(total, u0 + run);
+  const int2 range = chain_range(p.c, sh.plan, blockIdx.x);
+  const int u0 = range.x, u1 = range.y;
   if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");  // 168 a thread at launch: 128 threads give 64 each,
   else asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");            // 256 take 32 each
   if (warp < 8) tree_softmax<HD>(p, sh, q_smem, u0, u1);
@@ -704,7 +704,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) tree_attn_kernel(const __grid_c
   else if (warp == TAW_VALUES) tree_load<HD, true>(p, sh, v_ring, &vmap, u0, u1);
   else if (warp == TAW_MMA) tree_mma<HD>(p, sh, smem_u32(q_smem), smem_u32(k_ring), smem_u32(v_ring), u0, u1);
   else {
-    if (tid == TAW_CLEAR * 32) chain_describe(p.c, sh.plan, run, blockIdx.x, u0, u1, p.part.desc);
+    if (tid == TAW_CLEAR * 32) chain_describe(p.c, sh.plan, blockIdx.x, u0, u1, p.part.desc);
     __syncwarp();
     tree_clear<HD>(p, sh, smem_u32(v_ring));
   }
@@ -730,7 +730,7 @@ void launch_tree_attention(const RowsArgs& a, cudaStream_t st) {
     return;
   const int ctas = sm_count();
   TreeDev d;
-  d.c = chain_shape(a, TA_BLOCK, TA_TILE, TA_MIN_TILES);
+  d.c = chain_shape(a, TA_BLOCK, TA_TILE, TA_MIN_TILES, TA_PIECE_COST);
   d.Hq = sh.n_q_heads;
   d.scale_log2 = 1.4426950408889634f / sqrtf((float)sh.head_dim);
   d.mask = a.mask;
