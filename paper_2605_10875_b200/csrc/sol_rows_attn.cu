@@ -5,9 +5,10 @@
 //
 //   rows_attn_kernel   one CTA per SM takes its run of tiles (sol_chain.cuh; a tile is a 64-token page of one kv-head).  A
 //                      producer warp brings keys and values by TMA (128-byte swizzle) in steps of 16 KB, which the other
-//                      warps take in turn, each into its own ring of stages: 16 query rows are the M side of mma.sync
-//                      m16n8k16, online softmax in registers, weights as bf16 high and low parts.  At the end of a chain
-//                      the warps' results are merged through shared memory.
+//                      warps take in turn, each into its own ring of stages.  Tokens (then head_dim) are the M side of
+//                      mma.sync m16n8k16 and the query rows the N side, 16, 8 or 4 of them (S^T = K Q^T, O^T = V^T P^T);
+//                      online softmax in registers, weights as bf16 high and low parts, of four rows in one product.  At
+//                      the end of a chain the warps' results are merged through shared memory.
 //   rows_merge_kernel  merges the chains that were cut between CTAs.
 //   weight_kernel      the same for decode steps, and then the weights: w_t <- decay w_t + sum_g 2^(s_gt - lse_g) from the
 //                      logits that the first kernel left.
@@ -21,7 +22,7 @@
 
 namespace sol {
 
-constexpr int RA_ROWS = 16;   // query rows of a chain
+constexpr int RA_MAX_ROWS = 16;  // query rows of a chain at most
 constexpr int RA_WARPS = 6;   // consumer warps
 constexpr int RA_DEPTH = 2;   // stages of a warp's ring
 constexpr int RA_THREADS = (RA_WARPS + 1) * 32;
@@ -41,34 +42,37 @@ struct RowsDev {
   int* status;
 };
 
-// Tokens of a step (16 KB of keys and values), bytes of its keys, floats that a lane hands over in a merge.
-template <int HD>
+// ROWS query rows per chain: 16, 8 or 4.  Tokens of a step (16 KB of keys and values), bytes of its keys, floats that a lane hands
+// over in a merge.
+template <int HD, int ROWS>
 struct RaSize {
   static constexpr int TOK = HD == 64 ? 64 : 32;
   static constexpr int STEPS = PAGE / TOK;     // of a tile
   static constexpr int HALF = TOK * 128;       // a 64-wide half of the keys: [TOK tokens][128 B]
   static constexpr int TILE = HALF * (HD / 64);
   static constexpr int STAGES = RA_WARPS * RA_DEPTH;
-  static constexpr int REGS = HD / 8 * 4 + 4;  // sums, two maxima, two sums of weights
+  static constexpr int NB = ROWS == 16 ? 2 : 1;         // blocks of eight rows
+  static constexpr int REGS = (HD / 16 * 4 + 4) * NB;   // sums, two maxima, two sums of weights
   static constexpr int MERGE = 2 * REGS * 32 * 4;
   static constexpr int SMEM = 1024 + STAGES * 2 * TILE + MERGE;
 };
 
 // Shared-memory address of 16-byte piece c of token r of a step.
-template <int HD>
+template <int HALF>
 __device__ __forceinline__ uint32_t ra_piece(uint32_t base, int r, int c) {
-  return base + (uint32_t)((c >> 3) * RaSize<HD>::HALF + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+  return base + (uint32_t)((c >> 3) * HALF + r * 128 + (((c & 7) ^ (r & 7)) << 4));
 }
 __device__ __forceinline__ void ra_consumer_sync() {
   __syncwarp();
   asm volatile("bar.sync 1, %0;" ::"n"(RA_WARPS * 32) : "memory");
 }
 
-template <int HD>
+template <int HD, int ROWS>
 __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_constant__ CUtensorMap kmap,
                                                                   const __grid_constant__ CUtensorMap vmap, const RowsDev p) {
-  using Z = RaSize<HD>;
-  constexpr int KS = HD / 16, ND = HD / 8, NT = Z::TOK / 8;
+  using Z = RaSize<HD, ROWS>;
+  constexpr int KS = HD / 16, MT = Z::TOK / 16, NB = Z::NB;  // steps of head_dim, of tokens; blocks of eight rows
+  constexpr bool PACK = ROWS == 4;  // rows 4 .. 7 of the block are rows 0 .. 3 again: their weights' low parts
   extern __shared__ unsigned char ra_smem[];
   __shared__ ChainPlan plan;
   __shared__ uint64_t full[Z::STAGES], empty[Z::STAGES];
@@ -136,35 +140,46 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
   }
 
   // ---- the consumers ----
+  // a lane's share: tokens (or elements of the head) g and g + 8 of every 16, rows 2 t and 2 t + 1 of every block of eight
   const int g = lane >> 2, t = lane & 3, G = p.c.G;
   int it = 0;
   bool alive = true;
   for (int u = u0; u < u1;) {
     const ChainPiece c = chain_piece(p.c, plan, u, u1);
-    const int C = c.seq.T - c.seq.n, T = c.seq.T, rows = c.seq.n * G;
-    // this lane's rows: r0 = block * 16 + g and r0 + 8
-    uint32_t q[KS][4];
-    uint64_t seen[2];
-    const int r0 = c.block * RA_ROWS + g;
-    size_t base[2];
+    const int C = c.seq.T - c.seq.n, T = c.seq.T, rows = c.seq.n * G, row0 = c.block * ROWS;
+    auto row_at = [&](int r) {  // element of q and of the output where row r of the chain begins
+      const int node = (row0 + r) / G;
+      return (((size_t)c.b * p.c.max_nodes + node) * p.Hq + c.kvh * G + (row0 + r - node * G)) * HD;
+    };
+    uint32_t q[NB][KS][2];
+    uint64_t seen[NB][2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int r = r0 + 8 * h, node = r / G;
-      base[h] = (((size_t)c.b * p.c.max_nodes + node) * p.Hq + c.kvh * G + (r - node * G)) * HD;
-      seen[h] = r < rows ? (p.mask ? p.mask[(size_t)c.b * p.c.max_nodes + node] : ~0ull) : 0ull;
+    for (int nb = 0; nb < NB; ++nb) {
+      const int r = nb * 8 + (PACK ? g & 3 : g);
+      const bool real = row0 + r < rows;
+      const uint16_t* src = p.q + (real ? row_at(r) : 0);
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(p.q + base[h] + k * 16 + 2 * t);
-        q[k][h] = r < rows ? src[0] : 0u;
-        q[k][2 + h] = r < rows ? src[4] : 0u;
+        q[nb][k][0] = real ? *reinterpret_cast<const uint32_t*>(src + k * 16 + 2 * t) : 0u;
+        q[nb][k][1] = real ? *reinterpret_cast<const uint32_t*>(src + k * 16 + 8 + 2 * t) : 0u;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int col = nb * 8 + (PACK ? (2 * t + e) & 3 : 2 * t + e);
+        seen[nb][e] = row0 + col < rows ? (p.mask ? p.mask[(size_t)c.b * p.c.max_nodes + (row0 + col) / G] : ~0ull) : 0ull;
       }
     }
-    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
-    float o[ND][4];
+    float m[NB][2], l[NB][2], o[NB][KS][4];
 #pragma unroll
-    for (int j = 0; j < ND; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+    for (int nb = 0; nb < NB; ++nb) {
+      m[nb][0] = m[nb][1] = -INFINITY;
+      l[nb][0] = l[nb][1] = 0.f;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) o[nb][k][0] = o[nb][k][1] = o[nb][k][2] = o[nb][k][3] = 0.f;
+    }
 
     const int len = (c.tile1 - c.tile0) * Z::STEPS;
+#pragma unroll 1
     for (int x = (warp - it % RA_WARPS + RA_WARPS) % RA_WARPS; x < len; x += RA_WARPS) {
       const int use = (it + x) / RA_WARPS, st = warp * RA_DEPTH + use % RA_DEPTH;
       const int tok0 = c.tile0 * PAGE + x * Z::TOK;  // first token of the step
@@ -172,44 +187,49 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
       if (!alive) break;
       const uint32_t kb = smem_u32(ring + (size_t)st * 2 * Z::TILE), vb = kb + Z::TILE;
       const bool ok = page_ok[st] != 0;
-      float sc[NT][4];
+      float sc[NB][MT][4];
 #pragma unroll
-      for (int j = 0; j < NT; ++j) sc[j][0] = sc[j][1] = sc[j][2] = sc[j][3] = 0.f;
+      for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int k2 = 0; k2 < KS / 2; ++k2) {
+        for (int i = 0; i < MT; ++i) sc[nb][i][0] = sc[nb][i][1] = sc[nb][i][2] = sc[nb][i][3] = 0.f;
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          uint32_t bb[4];
-          ldsm_x4(bb, ra_piece<HD>(kb, j * 8 + (lane & 7), k2 * 4 + (lane >> 3)));
-          mma_bf16(sc[j], q[2 * k2][0], q[2 * k2][1], q[2 * k2][2], q[2 * k2][3], bb[0], bb[1]);
-          mma_bf16(sc[j], q[2 * k2 + 1][0], q[2 * k2 + 1][1], q[2 * k2 + 1][2], q[2 * k2 + 1][3], bb[2], bb[3]);
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          uint32_t a[4];
+          ldsm_x4(a, ra_piece<Z::HALF>(kb, i * 16 + (lane & 15), k * 2 + (lane >> 4)));
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) mma_bf16(sc[nb][i], a[0], a[1], a[2], a[3], q[nb][k][0], q[nb][k][1]);
         }
-      }
-      // ---- which tokens are seen; a tile inside the context is seen whole by every row ----
+      // ---- which tokens are seen; a step inside the context is seen whole by every row ----
       uint64_t bad = 0;  // drafted tokens of the step with values that are not finite
       if (ok && tok0 + Z::TOK <= C) {
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sc[j][e] *= p.scale_log2;
+          for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc[nb][i][e] *= p.scale_log2;
       } else {
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int tok = tok0 + j * 8 + 2 * t + (e & 1);
-            const bool s = ok && (tok < C || (tok < T && ((seen[e >> 1] >> (tok - C)) & 1)));
-            sc[j][e] = s ? sc[j][e] * p.scale_log2 : -INFINITY;
-          }
+          for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int tok = tok0 + i * 16 + g + (e >> 1) * 8;
+              const bool s = ok && (tok < C || (tok < T && ((seen[nb][e & 1] >> (tok - C)) & 1)));
+              sc[nb][i][e] = s ? sc[nb][i][e] * p.scale_log2 : -INFINITY;
+            }
         // A weight of zero must not meet a value that is not finite.  Rows of the page behind the sequence are cleared, and so
         // are drafted tokens' rows with such values, which are added below for the query rows that see them.
-#pragma unroll
+#pragma unroll 1
         for (int w = 0; w < Z::TOK / 32; ++w) {
           const int r = lane + 32 * w, tok = tok0 + r;
           bool drop = tok >= T || !ok;
           if (!drop && tok >= C) {
             for (int cc = 0; cc < HD / 8; ++cc) {
-              const uint4 v = lds128(ra_piece<HD>(vb, r, cc));
+              const uint4 v = lds128(ra_piece<Z::HALF>(vb, r, cc));
               const uint32_t x4[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
               for (int e = 0; e < 4; ++e)
@@ -218,73 +238,82 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
           }
           if (drop)
             for (int cc = 0; cc < HD / 8; ++cc)
-              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ra_piece<HD>(vb, r, cc)), "r"(0u) : "memory");
+              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ra_piece<Z::HALF>(vb, r, cc)), "r"(0u) : "memory");
           const uint32_t votes = __ballot_sync(0xffffffffu, drop && ok && tok >= C && tok < T);
           bad |= (uint64_t)votes << (32 * w);
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // ahead of the TMA write that takes the stage next
         __syncwarp();
       }
-      if (p.logits) {  // decode steps: the G heads are rows 0 .. G - 1
-        if (g < G) {
-          const size_t stride = (size_t)p.c.kv.max_pages_per_seq * PAGE;
-          float* dst = p.logits + (((size_t)c.b * p.c.Hkv + c.kvh) * G + g) * stride + tok0 + 2 * t;
+      if (p.logits) {  // decode steps: the G heads are the first rows
+        const size_t stride = (size_t)p.c.kv.max_pages_per_seq * PAGE;
+        float* dst = p.logits + ((size_t)c.b * p.c.Hkv + c.kvh) * G * stride + tok0 + g;
 #pragma unroll
-          for (int j = 0; j < NT; ++j) *reinterpret_cast<float2*>(dst + j * 8) = make_float2(sc[j][0], sc[j][1]);
+        for (int e = 0; e < 2; ++e)
+          if (2 * t + e < G) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+              dst[(2 * t + e) * stride + i * 16] = sc[0][i][e];
+              dst[(2 * t + e) * stride + i * 16 + 8] = sc[0][i][2 + e];
+            }
+          }
+      }
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        float f[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < MT; ++i) top = fmaxf(top, fmaxf(sc[nb][i][e], sc[nb][i][2 + e]));
+#pragma unroll
+          for (int off = 4; off <= 16; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+          const float now = fmaxf(m[nb][e], top), base = now == -INFINITY ? 0.f : now;  // a row that has seen nothing yet
+          f[e] = exp2f(m[nb][e] - base);
+          m[nb][e] = now;
+          l[nb][e] *= f[e];
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            sc[nb][i][e] = exp2f(sc[nb][i][e] - base);
+            sc[nb][i][2 + e] = exp2f(sc[nb][i][2 + e] - base);
+            l[nb][e] += sc[nb][i][e] + sc[nb][i][2 + e];
+          }
+        }
+        if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            o[nb][k][0] *= f[0];
+            o[nb][k][1] *= f[1];
+            o[nb][k][2] *= f[0];
+            o[nb][k][3] *= f[1];
+          }
         }
       }
-      float x0 = -INFINITY, x1 = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        x0 = fmaxf(x0, fmaxf(sc[j][0], sc[j][1]));
-        x1 = fmaxf(x1, fmaxf(sc[j][2], sc[j][3]));
-      }
+      for (int i = 0; i < MT; ++i) {
+        uint32_t hi[NB][2], lo[NB][2];  // the weights of 16 tokens, transposed
 #pragma unroll
-      for (int off = 1; off <= 2; off <<= 1) {
-        x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, off));
-        x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, off));
-      }
-      const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
-      const float b0 = n0 == -INFINITY ? 0.f : n0, b1 = n1 == -INFINITY ? 0.f : n1;  // a row that has seen nothing yet
-      const float f0 = exp2f(m0 - b0), f1 = exp2f(m1 - b1);
-      m0 = n0;
-      m1 = n1;
-      l0 *= f0;
-      l1 *= f1;
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int j = 0; j < ND; ++j) {
-        o[j][0] *= f0;
-        o[j][1] *= f0;
-        o[j][2] *= f1;
-        o[j][3] *= f1;
-      }
+          for (int h = 0; h < 2; ++h) {
+            const float v0 = sc[nb][i][2 * h], v1 = sc[nb][i][2 * h + 1];
+            const uint32_t w = pack_bf16(v0, v1), r = pack_bf16(v0 - bf16_lo(w), v1 - bf16_hi(w));
+            if (PACK) {
+              hi[nb][h] = movm_trans(t < 2 ? w : r);
+            } else {
+              hi[nb][h] = movm_trans(w);
+              lo[nb][h] = movm_trans(r);
+            }
+          }
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        sc[j][0] = exp2f(sc[j][0] - b0);
-        sc[j][1] = exp2f(sc[j][1] - b0);
-        sc[j][2] = exp2f(sc[j][2] - b1);
-        sc[j][3] = exp2f(sc[j][3] - b1);
-        l0 += sc[j][0] + sc[j][1];
-        l1 += sc[j][2] + sc[j][3];
-      }
+        for (int k = 0; k < KS; ++k) {
+          uint32_t a[4];
+          ldsm_x4_trans(a, ra_piece<Z::HALF>(vb, i * 16 + (lane & 7) + (lane >> 4) * 8, k * 2 + ((lane >> 3) & 1)));
 #pragma unroll
-      for (int kk = 0; kk < NT / 2; ++kk) {
-        uint32_t ph[4], pl[4];
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {  // n-tile 2 kk + (y >> 1), row half y & 1
-          const float v0 = sc[2 * kk + (y >> 1)][(y & 1) * 2], v1 = sc[2 * kk + (y >> 1)][(y & 1) * 2 + 1];
-          const uint16_t h0 = f2bf(v0), h1 = f2bf(v1);
-          ph[y] = (uint32_t)h0 | ((uint32_t)h1 << 16);
-          pl[y] = pack_bf16(v0 - bf2f(h0), v1 - bf2f(h1));
-        }
-#pragma unroll
-        for (int j2 = 0; j2 < ND / 2; ++j2) {
-          uint32_t bb[4];
-          ldsm_x4_trans(bb, ra_piece<HD>(vb, kk * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), j2 * 2 + (lane >> 4)));
-          mma_bf16(o[2 * j2], ph[0], ph[1], ph[2], ph[3], bb[0], bb[1]);
-          mma_bf16(o[2 * j2], pl[0], pl[1], pl[2], pl[3], bb[0], bb[1]);
-          mma_bf16(o[2 * j2 + 1], ph[0], ph[1], ph[2], ph[3], bb[2], bb[3]);
-          mma_bf16(o[2 * j2 + 1], pl[0], pl[1], pl[2], pl[3], bb[2], bb[3]);
+          for (int nb = 0; nb < NB; ++nb) {
+            mma_bf16(o[nb][k], a[0], a[1], a[2], a[3], hi[nb][0], hi[nb][1]);
+            if (!PACK) mma_bf16(o[nb][k], a[0], a[1], a[2], a[3], lo[nb][0], lo[nb][1]);
+          }
         }
       }
       if (bad) {  // p v in float32 for the rows that see such a token, from the cache
@@ -292,26 +321,23 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
         const uint16_t* v =
             static_cast<const uint16_t*>(p.c.kv.v_pool) + (((size_t)page * p.c.Hkv + c.kvh) * PAGE + tok0 % PAGE) * HD;
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+        for (int i = 0; i < MT; ++i)
+#pragma unroll 1
+          for (int j = 0; j < 16; ++j) {
+            const int tok = i * 16 + j;
+            if (!((bad >> tok) & 1)) continue;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {  // tokens 8 j + e: weights in lane e >> 1 of each quad
-            const float p0 = __shfl_sync(0xffffffffu, sc[j][e & 1], g * 4 + (e >> 1));
-            const float p1 = __shfl_sync(0xffffffffu, sc[j][2 + (e & 1)], g * 4 + (e >> 1));
-            if (!((bad >> (8 * j + e)) & 1)) continue;
-            const int node = tok0 + 8 * j + e - C;
-            const bool s0 = (seen[0] >> node) & 1, s1 = (seen[1] >> node) & 1;
+            for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int d = 0; d < ND; ++d) {
-              const uint32_t w = *reinterpret_cast<const uint32_t*>(v + (8 * j + e) * HD + d * 8 + 2 * t);
-              if (s0) {
-                o[d][0] += p0 * bf16_lo(w);
-                o[d][1] += p0 * bf16_hi(w);
+              for (int e = 0; e < 2; ++e) {
+                const float w = __shfl_sync(0xffffffffu, j < 8 ? sc[nb][i][e] : sc[nb][i][2 + e], (j & 7) * 4 + t);
+                if (!((seen[nb][e] >> (tok0 + tok - C)) & 1) || (PACK && t >= 2)) continue;
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                  o[nb][k][e] += w * bf2f(v[tok * HD + k * 16 + g]);
+                  o[nb][k][2 + e] += w * bf2f(v[tok * HD + k * 16 + 8 + g]);
+                }
               }
-              if (s1) {
-                o[d][2] += p1 * bf16_lo(w);
-                o[d][3] += p1 * bf16_hi(w);
-              }
-            }
           }
       }
       __syncwarp();
@@ -326,59 +352,77 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
       const bool gives = warp >= half && warp < min(2 * half, RA_WARPS), takes = warp + half < min(2 * half, RA_WARPS);
       if (gives) {
 #pragma unroll
-        for (int j = 0; j < ND; ++j)
+        for (int nb = 0; nb < NB; ++nb) {
+          float* s = slot + nb * (KS * 4 + 4) * 32;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) slot[(j * 4 + e) * 32] = o[j][e];
-        slot[(ND * 4) * 32] = m0;
-        slot[(ND * 4 + 1) * 32] = m1;
-        slot[(ND * 4 + 2) * 32] = l0;
-        slot[(ND * 4 + 3) * 32] = l1;
+          for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[(k * 4 + e) * 32] = o[nb][k][e];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            s[(KS * 4 + e) * 32] = m[nb][e];
+            s[(KS * 4 + 2 + e) * 32] = l[nb][e];
+          }
+        }
       }
       ra_consumer_sync();
       if (takes) {
-        const float y0 = slot[(ND * 4) * 32], y1 = slot[(ND * 4 + 1) * 32];
-        const float n0 = fmaxf(m0, y0), n1 = fmaxf(m1, y1);
-        const float b0 = n0 == -INFINITY ? 0.f : n0, b1 = n1 == -INFINITY ? 0.f : n1;
-        const float f0 = exp2f(m0 - b0), f1 = exp2f(m1 - b1), h0 = exp2f(y0 - b0), h1 = exp2f(y1 - b1);
-        m0 = n0;
-        m1 = n1;
-        l0 = l0 * f0 + slot[(ND * 4 + 2) * 32] * h0;
-        l1 = l1 * f1 + slot[(ND * 4 + 3) * 32] * h1;
 #pragma unroll
-        for (int j = 0; j < ND; ++j) {
-          o[j][0] = o[j][0] * f0 + slot[(j * 4) * 32] * h0;
-          o[j][1] = o[j][1] * f0 + slot[(j * 4 + 1) * 32] * h0;
-          o[j][2] = o[j][2] * f1 + slot[(j * 4 + 2) * 32] * h1;
-          o[j][3] = o[j][3] * f1 + slot[(j * 4 + 3) * 32] * h1;
+        for (int nb = 0; nb < NB; ++nb) {
+          const float* s = slot + nb * (KS * 4 + 4) * 32;
+          float f[2], h[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float y = s[(KS * 4 + e) * 32], now = fmaxf(m[nb][e], y), base = now == -INFINITY ? 0.f : now;
+            f[e] = exp2f(m[nb][e] - base);
+            h[e] = exp2f(y - base);
+            m[nb][e] = now;
+            l[nb][e] = l[nb][e] * f[e] + s[(KS * 4 + 2 + e) * 32] * h[e];
+          }
+#pragma unroll
+          for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[nb][k][e] = o[nb][k][e] * f[e & 1] + s[(k * 4 + e) * 32] * h[e & 1];
         }
       }
       ra_consumer_sync();
     }
     if (warp == 0) {
-#pragma unroll
-      for (int off = 1; off <= 2; off <<= 1) {
-        l0 += __shfl_xor_sync(0xffffffffu, l0, off);
-        l1 += __shfl_xor_sync(0xffffffffu, l1, off);
-      }
       const bool whole = c.whole();
-      const size_t part = (size_t)(2 * blockIdx.x + (u > u0)) * p.part.rows + g;
+      const size_t part = (size_t)(2 * blockIdx.x + (u > u0)) * p.part.rows;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int r = r0 + 8 * h;
-        if (r >= rows) continue;
-        const float l = h ? l1 : l0, m = h ? m1 : m0;
-        if (whole) {
-          const float inv = l == 0.f ? 0.f : 1.0f / l;
+      for (int nb = 0; nb < NB; ++nb) {
+        if (PACK) {  // high and low parts
 #pragma unroll
-          for (int j = 0; j < ND; ++j)
-            *reinterpret_cast<uint32_t*>(p.out + base[h] + j * 8 + 2 * t) = pack_bf16(o[j][2 * h] * inv, o[j][2 * h + 1] * inv);
-          if (p.lse && t == 0) p.lse[(size_t)c.b * p.Hq + c.kvh * G + r] = l == 0.f ? INFINITY : m + log2f(l);
-        } else {
-          float* dst = p.part.sums + (part + 8 * h) * HD;
+          for (int k = 0; k < KS; ++k)
 #pragma unroll
-          for (int j = 0; j < ND; ++j)
-            *reinterpret_cast<float2*>(dst + j * 8 + 2 * t) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
-          if (t == 0) p.part.ml[part + 8 * h] = make_float2(m, l);
+            for (int e = 0; e < 4; ++e) o[nb][k][e] += __shfl_xor_sync(0xffffffffu, o[nb][k][e], 2);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float sum = l[nb][e];
+#pragma unroll
+          for (int off = 4; off <= 16; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+          const int r = nb * 8 + 2 * t + e;
+          if (row0 + r >= rows || (PACK && t >= 2)) continue;
+          if (whole) {
+            const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+            uint16_t* dst = p.out + row_at(r) + g;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+              dst[k * 16] = f2bf(o[nb][k][e] * inv);
+              dst[k * 16 + 8] = f2bf(o[nb][k][2 + e] * inv);
+            }
+            if (p.lse && g == 0) p.lse[(size_t)c.b * p.Hq + c.kvh * G + r] = sum == 0.f ? INFINITY : m[nb][e] + log2f(sum);
+          } else {
+            float* dst = p.part.sums + (part + r) * HD + g;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+              dst[k * 16] = o[nb][k][e];
+              dst[k * 16 + 8] = o[nb][k][2 + e];
+            }
+            if (g == 0) p.part.ml[part + r] = make_float2(m[nb][e], sum);
+          }
         }
       }
     }
@@ -483,30 +527,32 @@ __global__ void __launch_bounds__(RM_THREADS) weight_kernel(const RowsDev p, int
 }
 
 // ---- host ----------------------------------------------------------------------------------------
-size_t rows_part_bytes(const sol_shape_t& sh) { return chain_part_bytes(sm_count(), RA_ROWS, sh.head_dim); }
+static int rows_of_chain(int rows) { return rows <= 4 ? 4 : rows <= 8 ? 8 : 16; }
+size_t rows_part_bytes(const sol_shape_t& sh) { return chain_part_bytes(sm_count(), RA_MAX_ROWS, sh.head_dim); }
 
-template <int HD>
-static void launch_rows(RowsDev d, const CUtensorMap& kmap, const CUtensorMap& vmap, const RowsArgs& a, cudaStream_t st) {
+template <int HD, int ROWS>
+static void launch_rows(RowsDev d, const RowsArgs& a, cudaStream_t st) {
+  using Z = RaSize<HD, ROWS>;
+  CUtensorMap kmap, vmap;
+  if (!encode_pool_map(&kmap, a.kv.k_pool, a.shape, a.kv.num_pages, Z::TOK) ||
+      !encode_pool_map(&vmap, a.kv.v_pool, a.shape, a.kv.num_pages, Z::TOK))
+    return;
   // fewer CTAs where the caller's space for partial results is short
-  const int rows = a.weights ? d.c.G : RA_ROWS;
+  const int rows = std::min(ROWS, d.c.max_nodes * d.c.G);
   const int ctas = (int)std::min<size_t>(sm_count(), a.part_bytes / chain_part_bytes(1, rows, HD));
   d.part = chain_parts(a.part, ctas, rows, HD);
-  ensure_dynamic_smem(reinterpret_cast<const void*>(&rows_attn_kernel<HD>), RaSize<HD>::SMEM);
-  SOL_LAUNCH("rows_attn", rows_attn_kernel<HD>, dim3(ctas), dim3(RA_THREADS), RaSize<HD>::SMEM, st, kmap, vmap, d);
+  ensure_dynamic_smem(reinterpret_cast<const void*>(&rows_attn_kernel<HD, ROWS>), Z::SMEM);
+  SOL_LAUNCH("rows_attn", (rows_attn_kernel<HD, ROWS>), dim3(ctas), dim3(RA_THREADS), Z::SMEM, st, kmap, vmap, d);
   if (a.weights) SOL_LAUNCH("attn_weights", weight_kernel<HD>, dim3(4 * ctas), dim3(RM_THREADS), 0, st, d, ctas, a.decay, a.weights);
   else launch_chain_merge(d.c, d.part, d.Hq, HD, ctas, d.out, st);
 }
 
 void launch_rows_attention(const RowsArgs& a, cudaStream_t st) {
   const sol_shape_t& sh = a.shape;
-  CUtensorMap kmap, vmap;
-  const int box = sh.head_dim == 64 ? RaSize<64>::TOK : RaSize<128>::TOK;
-  if (!encode_pool_map(&kmap, a.kv.k_pool, sh, a.kv.num_pages, box) ||
-      !encode_pool_map(&vmap, a.kv.v_pool, sh, a.kv.num_pages, box))
-    return;
+  const int rows = rows_of_chain(a.max_nodes * (sh.n_q_heads / sh.n_kv_heads));
   RowsDev d;
   memset(&d, 0, sizeof(d));
-  d.c = chain_shape(a, RA_ROWS, PAGE, RA_MIN_TILES, RA_PIECE_COST);
+  d.c = chain_shape(a, rows, PAGE, RA_MIN_TILES, RA_PIECE_COST);
   d.Hq = sh.n_q_heads;
   d.scale_log2 = 1.4426950408889634f / sqrtf((float)sh.head_dim);
   d.mask = a.mask;
@@ -515,8 +561,15 @@ void launch_rows_attention(const RowsArgs& a, cudaStream_t st) {
   d.logits = a.weights ? a.logits : nullptr;
   d.lse = a.weights ? a.lse : nullptr;
   d.status = a.status;
-  if (sh.head_dim == 64) launch_rows<64>(d, kmap, vmap, a, st);
-  else launch_rows<128>(d, kmap, vmap, a, st);
+  if (sh.head_dim == 64) {
+    if (rows == 4) launch_rows<64, 4>(d, a, st);
+    else if (rows == 8) launch_rows<64, 8>(d, a, st);
+    else launch_rows<64, 16>(d, a, st);
+  } else {
+    if (rows == 4) launch_rows<128, 4>(d, a, st);
+    else if (rows == 8) launch_rows<128, 8>(d, a, st);
+    else launch_rows<128, 16>(d, a, st);
+  }
 }
 
 }  // namespace sol
