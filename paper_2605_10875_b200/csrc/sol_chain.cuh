@@ -4,10 +4,12 @@
 // A chain is what one softmax runs along: a (sequence, kv-head, block of query rows) over the sequence's tokens, a tile of one
 // or two cache pages at a time.  The tiles of all chains, one chain after the other, form one line, of which every CTA takes a
 // run.  A run that ends inside a chain leaves a partial result; a second kernel merges the pieces of chains that were cut.
-// Two ways to cut, of which every CTA works out for itself, from the lengths (at most 128), which one is the better:
+// A chain has piece_cost places on the line ahead of its tiles, as many tiles as beginning and ending a piece is worth, so that
+// runs of many short chains are not the longest (128 ragged sequences: 394 us without, 330 with).  Two ways to cut, of which
+// every CTA works out for itself, from the lengths (at most 128), which one is the better:
 //   equal runs       whatever the lengths are.  A run covers the end of one chain, some whole chains and the beginning of another
-//   CTAs per chain   in proportion to its tiles, one at least: every CTA has one piece.  Taken if that costs no more than the
-//                    second piece that equal runs give most CTAs (beginning and ending a piece takes as long as piece_cost tiles)
+//   CTAs per chain   in proportion to its tiles, one at least: every CTA has one piece.  Taken if none is much longer than an equal
+//                    run, where a CTA has the end of one chain and the beginning of another
 #pragma once
 #include "sol_common.cuh"
 #include "sol_internal.h"
@@ -47,11 +49,11 @@ struct ChainShape {
 
 // The line of tiles.
 struct ChainPlan {
-  int cum[CHAIN_MAX_BATCH + 1];    // tiles of the sequences before b
+  int cum[CHAIN_MAX_BATCH + 1];    // places of the sequences before b
   int first[CHAIN_MAX_BATCH + 1];  // CTAs per chain: CTAs of the sequences before b
   uint32_t seq[CHAIN_MAX_BATCH];   // T << 8 | n
   int wsum[8];
-  int run;                         // equal runs: tiles of each; 0: CTAs per chain
+  int run;                         // equal runs: places of each; 0: CTAs per chain
   __device__ __forceinline__ ChainSeq at(int b) const {
     ChainSeq s;
     s.T = (int)(seq[b] >> 8);
@@ -105,17 +107,18 @@ __device__ __forceinline__ void chain_plan(const ChainShape& c, ChainPlan& p, in
   if (tid < c.B) s = chain_seq(c.kv, c.n_nodes, c.max_nodes, tid, status);
   if (tid < CHAIN_MAX_BATCH) p.seq[tid] = (uint32_t)s.T << 8 | (uint32_t)s.n;
   const int chains = s.n > 0 ? chain_blocks(c, s) * c.Hkv : 0, tiles = chain_tiles(c, s);
-  scan(tiles * chains, p.cum);
+  const int places = tiles + c.piece_cost;
+  scan(places * chains, p.cum);
   const int total = p.cum[c.B], run = max(c.min_tiles, (total + ctas - 1) / ctas);
-  const int share = max(1, (int)((long long)tiles * ctas / max(total, 1)));  // CTAs of each of the sequence's chains
+  const int share = max(1, (int)((long long)places * ctas / max(total, 1)));  // CTAs of each of the sequence's chains
   const int give = min(share, max(1, tiles / c.min_tiles));
   scan(give * chains, p.first);
-  const int worst = __syncthreads_or(chains > 0 && (tiles + give - 1) / give > run + c.piece_cost);
+  const int worst = __syncthreads_or(chains > 0 && (tiles + give - 1) / give > run + c.piece_cost / 2);
   if (tid == 0) p.run = worst || p.first[c.B] > ctas ? run : 0;
   __syncthreads();
 }
 
-// The sequence that holds tile u of the line.
+// The sequence that holds place u of the line.
 __device__ __forceinline__ int chain_find(const ChainShape& c, const ChainPlan& p, int u) {
   int lo = 0, hi = c.B - 1;
   while (lo < hi) {
@@ -126,12 +129,17 @@ __device__ __forceinline__ int chain_find(const ChainShape& c, const ChainPlan& 
   return lo;
 }
 
-// The run of tiles [u0, u1) of a CTA.
+// The run [u0, u1) of a CTA, empty or with a tile at its end.
 __device__ __forceinline__ int2 chain_range(const ChainShape& c, const ChainPlan& p, int cta) {
   const int total = p.cum[c.B];
   if (p.run) {
     const int u0 = (int)min((long long)cta * p.run, (long long)total);
-    return make_int2(u0, min(total, u0 + p.run));
+    int u1 = min(total, u0 + p.run);
+    if (u0 < u1) {  // what it holds of a chain's places ahead of the tiles, at its end, is nothing
+      const int b = chain_find(c, p, u1 - 1), places = chain_tiles(c, p.at(b)) + c.piece_cost, at = (u1 - p.cum[b]) % places;
+      if (at && at <= c.piece_cost) u1 -= at;
+    }
+    return make_int2(u0, max(u0, u1));
   }
   if (cta >= p.first[c.B]) return make_int2(total, total);
   int lo = 0, hi = c.B - 1;
@@ -142,7 +150,8 @@ __device__ __forceinline__ int2 chain_range(const ChainShape& c, const ChainPlan
   }
   const ChainSeq s = p.at(lo);
   const int tiles = chain_tiles(c, s), each = (p.first[lo + 1] - p.first[lo]) / (chain_blocks(c, s) * c.Hkv);
-  const int local = cta - p.first[lo], chain = local / each, i = local - chain * each, base = p.cum[lo] + chain * tiles;
+  const int local = cta - p.first[lo], chain = local / each, i = local - chain * each;
+  const int base = p.cum[lo] + chain * (tiles + c.piece_cost) + c.piece_cost;
   return make_int2(base + (int)((long long)tiles * i / each), base + (int)((long long)tiles * (i + 1) / each));
 }
 
@@ -150,6 +159,7 @@ __device__ __forceinline__ int2 chain_range(const ChainShape& c, const ChainPlan
 struct ChainPiece {
   int b, kvh, block;
   int tile0, tile1, tiles;  // tiles: of the whole chain
+  int next;                 // place where the run goes on
   ChainSeq seq;
   __device__ __forceinline__ bool whole() const { return tile0 == 0 && tile1 == tiles; }
 };
@@ -158,9 +168,11 @@ __device__ __forceinline__ ChainPiece chain_piece(const ChainShape& c, const Cha
   r.b = chain_find(c, p, u);
   r.seq = p.at(r.b);
   r.tiles = chain_tiles(c, r.seq);
-  const int local = u - p.cum[r.b], chain = local / r.tiles, blocks = chain_blocks(c, r.seq);
-  r.tile0 = local - chain * r.tiles;
-  r.tile1 = min(r.tiles, r.tile0 + end - u);
+  const int places = r.tiles + c.piece_cost, local = u - p.cum[r.b], chain = local / places, blocks = chain_blocks(c, r.seq);
+  const int at = local - chain * places, to = min(places, at + end - u);
+  r.tile0 = max(0, at - c.piece_cost);
+  r.tile1 = to - c.piece_cost;
+  r.next = u + to - at;
   r.kvh = chain / blocks;
   r.block = chain - r.kvh * blocks;
   return r;
@@ -178,10 +190,10 @@ __device__ __forceinline__ ChainCut chain_cut(const ChainShape& c, const ChainPl
   const ChainSeq s = p.at(b);
   ChainCut r;
   if (p.run) {
-    const int tiles = chain_tiles(c, s), u0 = p.cum[b] + chain * tiles;
+    const int tiles = chain_tiles(c, s), base = p.cum[b] + chain * (tiles + c.piece_cost), u0 = base + c.piece_cost;
     r.first = u0 / p.run;
     r.last = (u0 + tiles - 1) / p.run;
-    r.first_slot = 2 * r.first + (u0 % p.run ? 1 : 0);
+    r.first_slot = 2 * r.first + (base > r.first * p.run ? 1 : 0);
   } else {
     const int each = (p.first[b + 1] - p.first[b]) / (chain_blocks(c, s) * c.Hkv);
     r.first = p.first[b] + chain * each;

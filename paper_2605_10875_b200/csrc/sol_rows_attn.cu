@@ -27,7 +27,7 @@ constexpr int RA_WARPS = 6;   // consumer warps
 constexpr int RA_DEPTH = 2;   // stages of a warp's ring
 constexpr int RA_THREADS = (RA_WARPS + 1) * 32;
 constexpr int RA_MIN_TILES = 4;
-constexpr int RA_PIECE_COST = 8;
+constexpr int ra_piece_cost(int hd) { return hd == 64 ? 8 : 4; }
 
 struct RowsDev {
   ChainShape c;
@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
           __syncwarp();
         }
       }
-      u += c.tile1 - c.tile0;
+      u = c.next;
     }
     return;
   }
@@ -426,7 +426,7 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
         }
       }
     }
-    u += c.tile1 - c.tile0;
+    u = c.next;
   }
 }
 
@@ -552,7 +552,7 @@ void launch_rows_attention(const RowsArgs& a, cudaStream_t st) {
   const int rows = rows_of_chain(a.max_nodes * (sh.n_q_heads / sh.n_kv_heads));
   RowsDev d;
   memset(&d, 0, sizeof(d));
-  d.c = chain_shape(a, rows, PAGE, RA_MIN_TILES, RA_PIECE_COST);
+  d.c = chain_shape(a, rows, PAGE, RA_MIN_TILES, ra_piece_cost(sh.head_dim));
   d.Hq = sh.n_q_heads;
   d.scale_log2 = 1.4426950408889634f / sqrtf((float)sh.head_dim);
   d.mask = a.mask;

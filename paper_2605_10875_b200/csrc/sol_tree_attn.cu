@@ -33,7 +33,7 @@ constexpr int TA_ROWS = 128;            // lanes of a unit
 constexpr int TA_BLOCK = 2 * TA_ROWS;   // rows of a chain
 constexpr int TA_TILE = 2 * PAGE;       // tokens of a tile
 constexpr int TA_MIN_TILES = 2;
-constexpr int TA_PIECE_COST = 6;
+constexpr int ta_piece_cost(int hd) { return hd == 64 ? 8 : 4; }
 constexpr int TA_THREADS = 12 * 32;
 constexpr float TA_SLACK = 8.f;         // weights reach 2^8 before the maximum moves
 constexpr int TA_EX = 32;               // columns handed over at a time at the end of a piece
@@ -192,7 +192,7 @@ __device__ void tree_load(const TreeDev& p, TreeShared<HD>& sh, unsigned char* r
         phase ^= 1;
       }
     }
-    u += c.steps;
+    u = c.next;
   }
   if (!alive)  // a wait gave up: what has been requested still arrives before the CTA ends
     for (int i = max(0, n - SLOTS); i < n; ++i) mbar_wait(&full[i % SLOTS], (i / SLOTS) & 1, p.status);
@@ -386,7 +386,7 @@ __device__ void tree_mma(const TreeDev& p, TreeShared<HD>& sh, uint32_t q_oper, 
         if (more) k_step();
       }
     }
-    u += steps;
+    u = c.next;
   }
 }
 
@@ -579,7 +579,7 @@ __device__ void tree_softmax(const TreeDev& p, TreeShared<HD>& sh, unsigned char
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.p_ready[unit]);
     }
-    const int u_next = u + c.steps;
+    const int u_next = c.next;
     TreePiece next = c;
     if (u_next < u1) {  // the next queries on their way to L2 while this piece ends
       next = tree_piece(p.c, sh.plan, u_next, u1);
@@ -730,7 +730,7 @@ void launch_tree_attention(const RowsArgs& a, cudaStream_t st) {
     return;
   const int ctas = sm_count();
   TreeDev d;
-  d.c = chain_shape(a, TA_BLOCK, TA_TILE, TA_MIN_TILES, TA_PIECE_COST);
+  d.c = chain_shape(a, TA_BLOCK, TA_TILE, TA_MIN_TILES, ta_piece_cost(sh.head_dim));
   d.Hq = sh.n_q_heads;
   d.scale_log2 = 1.4426950408889634f / sqrtf((float)sh.head_dim);
   d.mask = a.mask;
