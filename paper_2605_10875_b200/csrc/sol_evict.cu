@@ -1,11 +1,13 @@
 // Eviction: of every (sequence, kv-head) the budget's tokens of largest accumulated weight stay, and move together in order.
 //
-//   evict_select_kernel  a CTA per (sequence, kv-head): the row's weights as sortable keys in shared memory, radix select of the
-//                        budget's last one (sol_select.cuh), ascending list of the kept tokens
-//   evict_move_kernel    rows of keys and values to their new slots, the weights with them.  A key moves from position i to
-//                        position j <= i and is rotated by j - i, so that slot t keeps a key at position t, which is where the
-//                        decode step will put its queries and the next key.
+//   evict_select_kernel  a CTA per (sequence, kv-head): the row's weights in shared memory, radix select of the budget's last one
+//                        (sol_select.cuh), ascending list of the kept tokens, their weights moved together
+//   evict_move_kernel    rows of keys and values to their new slots.  A key moves from position i to position j <= i and is
+//                        rotated by j - i, so that slot t keeps a key at position t, which is where the decode step will put
+//                        its queries and the next key.
 #include <math.h>
+
+#include <algorithm>
 
 #include "sol_common.cuh"
 #include "sol_internal.h"
@@ -63,33 +65,40 @@ __global__ void __launch_bounds__(ES_THREADS) evict_select_kernel(const EvictArg
   const EvictPlan e = evict_plan(p, b);
   const size_t stride = (size_t)p.kv.max_pages_per_seq * PAGE, row = ((size_t)b * p.shape.n_kv_heads + kvh) * stride;
   int32_t* out = p.kept_idx + row;
-  if (e.k >= e.T) {
-    for (int i = tid; i < e.T; i += ES_THREADS) out[i] = i;
+  if (kvh == 0 && tid == 0) p.dst_lens[b] = e.k;
+  constexpr int L = 8;  // loads in flight
+  auto weights = [&](auto take) {  // take(i, weight of token i), a token per thread
+#pragma unroll 1
+    for (int i0 = tid; i0 < e.T; i0 += L * ES_THREADS) {
+      float w[L];
+#pragma unroll
+      for (int x = 0; x < L; ++x) w[x] = i0 + x * ES_THREADS < e.T ? p.weights[row + i0 + x * ES_THREADS] : 0.f;
+#pragma unroll
+      for (int x = 0; x < L; ++x)
+        if (i0 + x * ES_THREADS < e.T) take(i0 + x * ES_THREADS, w[x]);
+    }
+  };
+  if (e.k >= e.T) {  // all stay
+    weights([&](int i, float w) {
+      out[i] = i;
+      p.dst_weights[row + i] = w;
+    });
     return;
   }
-  // Forced tokens have the largest key; a weight that is no number counts less than any.
-  const int per = ((e.T + ES_THREADS - 1) / ES_THREADS) | 1;  // odd: the threads' runs start in different banks
-  constexpr int L = 8;  // loads in flight
-#pragma unroll 1
-  for (int i0 = tid; i0 < per * ES_THREADS; i0 += L * ES_THREADS) {
-    float w[L];
-#pragma unroll
-    for (int x = 0; x < L; ++x) w[x] = i0 + x * ES_THREADS < e.T ? p.weights[row + i0 + x * ES_THREADS] + 0.f : 0.f;  // one zero
-#pragma unroll
-    for (int x = 0; x < L; ++x) {
-      const int i = i0 + x * ES_THREADS;
-      uint32_t key = w[x] == w[x] ? float_key(w[x]) : 1u;
-      if (i < e.sinks || i >= e.T - e.window) key = i < e.T ? 0xffffffffu : 0u;
-      if (i < per * ES_THREADS) es_keys[i] = key;
-    }
-  }
-  __syncthreads();
   if (e.k <= 0) return;
+  // Forced tokens have the largest key; a weight that is no number counts less than any; there is one zero.
+  const int per = ((e.T + ES_THREADS - 1) / ES_THREADS) | 1;  // odd: the threads' runs start in different banks
+  weights([&](int i, float w) {
+    es_keys[i] = i < e.sinks || i >= e.T - e.window ? 0xffffffffu : w == w ? float_key(w + 0.f) : 1u;
+  });
+  for (int i = e.T + tid; i < per * ES_THREADS; i += ES_THREADS) es_keys[i] = 0;
+  __syncthreads();
   int ties = 0;
   const uint32_t kth = select_kth<ES_THREADS, 0, true>([&](int i) { return es_keys[tid * per + i]; }, e.k, ties, sm, per);
   __syncthreads();
   // kept before this thread's run: those above the k-th, and of its equals the first `ties`
   int above = 0, equal = 0;
+#pragma unroll 4
   for (int i = 0; i < per; ++i) {
     const uint32_t key = es_keys[tid * per + i];
     above += key > kth;
@@ -116,10 +125,18 @@ __global__ void __launch_bounds__(ES_THREADS) evict_select_kernel(const EvictArg
     q += sm.scan[1][w];
   }
   int at = a + min(q, ties);
+#pragma unroll 4
   for (int i = 0; i < per; ++i) {
     const uint32_t key = es_keys[tid * per + i];
     if (key > kth || (key == kth && q++ < ties)) out[at++] = tid * per + i;
   }
+  __syncthreads();
+  // the weights follow, by way of the keys' place: in place, too, they are all read before one is written
+  float* held = reinterpret_cast<float*>(es_keys);
+  weights([&](int i, float w) { held[i] = w; });
+  __syncthreads();
+#pragma unroll 4
+  for (int j = tid; j < e.k; j += ES_THREADS) p.dst_weights[row + j] = held[out[j]];
 }
 
 // ---- the move ------------------------------------------------------------------------------------
@@ -148,130 +165,258 @@ __device__ __forceinline__ float2 turn_back(uint32_t back, uint2 speed) {
                      __uint_as_float(__float_as_uint(sin_) ^ (quarter & 0x80000000u)));
 }
 
-// A CTA takes `1 / slabs` of the 16-byte pieces of every kept row of a (sequence, kv-head)'s keys or values, a lane per piece and
-// U rows per lane at a time: read, then written, in order.  In place this is safe: row j goes to slot j and kept_idx[j] >= j,
-// so what a write covers is a row that has been read, and no other CTA touches these pieces.  Keys: the low lanes of a row hold
-// pieces of its first half, the high ones the pieces that are rotated with them; each rotates four of the eight pairs.  The last
-// CTA of a (sequence, kv-head) moves the weights, a token per thread.
-// Bound by memory latency times rows in flight: whole rows where the batch fills the chip, otherwise slabs of 64 bytes, and more
-// threads where there are few CTAs.
-constexpr int EM_ROWS = 4;  // U
+// A CTA moves `1 / slabs` of every kept row of a (sequence, kv-head)'s keys or values, chunks of 32 slabs rows through a ring in
+// shared memory: up to eight warps request chunks in turn, 16 bytes a lane, eight write them out in turn.  In place this is safe: row j
+// goes to slot j and kept_idx[j] >= j, so what the write of a chunk covers is a row of that chunk or an earlier one, and a warp
+// writes a chunk only after it has seen that chunk and all before it arrive; what is requested later lies behind every slot
+// written so far; and no other CTA touches these pieces.
+// Keys: a slab of a row is a piece of its first half and the piece that is rotated with it, eight pairs per lane.  How far a row
+// moves back never falls from one row to the next and hardly changes within a chunk, so its angle is put together from two tables
+// in shared memory, of 0 .. 63 positions and of the chunk's few multiples of 64 (an angle from the polynomials for every pair takes
+// three times the instructions); chunks that span more have their angles from the polynomials.
+// Bound by HBM for batches, by the latency of a chunk times the chunks of the longest sequence otherwise.  (Rows read into
+// registers, between barriers, took 4 us a round, 317 us for half of 24 ragged caches; bulk copies of single rows 25 to 40 ns
+// each, 1447 us.)
+constexpr int EM_READERS = 8, EM_WRITERS = 8;  // warps
+constexpr int EM_THREADS = (EM_READERS + EM_WRITERS) * 32;
+constexpr int EM_FAR = 4;          // multiples of 64 positions in a chunk's table
+constexpr int EM_MAX_STAGES = 24;
+
+struct MoveShape {
+  int slabs, stages;
+  uint2 speeds[64];  // turns per position of a head's pairs, as 64-bit fractions: low, high word
+};
+// Shared memory of a stage: the rows, where each comes from, goes to and how far it moves, angles of EM_FAR multiples of 64.
+__host__ __device__ constexpr int em_far_bytes(int hd, int slabs) { return EM_FAR * 2 * (hd / 2 / slabs) * 4; }
+__host__ __device__ constexpr int em_stage_bytes(int hd, int slabs) { return 32 * hd * 2 + 32 * slabs * (8 + 8 + 4) + em_far_bytes(hd, slabs); }
+
+__device__ __forceinline__ void em_copy16(uint32_t dst_smem, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst_smem), "l"(src) : "memory");
+}
+
+__device__ __forceinline__ uint32_t em_pack(float lo, float hi) {
+  uint32_t y;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
+  return y;
+}
+
 template <int HD>
-__global__ void __launch_bounds__(1024) evict_move_kernel(const EvictArgs p, int slabs) {
-  constexpr int PPR = HD / 8, U = EM_ROWS;
-  __shared__ uint2 speeds[HD / 2];  // turns per position: low, high word
-  const int kvh = blockIdx.y, tid = threadIdx.x, threads = blockDim.x;
+__global__ void __launch_bounds__(EM_THREADS) evict_move_kernel(const EvictArgs p, const MoveShape sh) {
+  constexpr int ROW = HD * 2;      // bytes of a row
+  constexpr int CHUNK = 32 * ROW;  // bytes of a chunk: 32 slabs rows of ROW / slabs bytes
+  extern __shared__ __align__(128) unsigned char em_smem[];
+  __shared__ uint64_t full[EM_MAX_STAGES], empty[EM_MAX_STAGES];
+  __shared__ uint2 speeds[HD / 2];   // of the slab
+  __shared__ int far0[EM_MAX_STAGES];  // first multiple of 64 in the stage's table; -1: its angles are in no table
+  const int slabs = sh.slabs, stages = sh.stages, rows = 32 * slabs, bytes = ROW / slabs, F = HD / 2 / slabs;
+  const int kvh = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int Hkv = p.shape.n_kv_heads, mp = p.kv.max_pages_per_seq;
   const bool keys = blockIdx.x < slabs, rope = keys && p.shape.rope_theta > 0.f;
-  if (rope && tid < HD / 2) {
-    const double turns = exp2(-2.0 * tid / HD * log2((double)p.shape.rope_theta)) * 0.15915494309189535;  // of one position
-    const uint64_t fraction = (uint64_t)((turns - floor(turns)) * 0x1p64);
-    speeds[tid] = make_uint2((uint32_t)fraction, (uint32_t)(fraction >> 32));
+  const int slab = keys ? blockIdx.x : blockIdx.x - slabs;
+  float* near = reinterpret_cast<float*>(em_smem);  // [64][2][F] cosines, sines
+  unsigned char* stage0 = em_smem + 64 * 2 * F * 4;
+  const int stage_bytes = em_stage_bytes(HD, slabs);
+  struct Stage {
+    unsigned char* data;
+    unsigned char **src, **dst;  // nullptr: nothing to move
+    int* back;
+    float* far;
+  };
+  auto stage = [&](int st) {
+    Stage s;
+    s.data = stage0 + (size_t)st * stage_bytes;
+    s.far = reinterpret_cast<float*>(s.data + CHUNK);
+    s.src = reinterpret_cast<unsigned char**>(s.data + CHUNK + em_far_bytes(HD, slabs));
+    s.dst = s.src + rows;
+    s.back = reinterpret_cast<int*>(s.dst + rows);
+    return s;
+  };
+  if (rope && tid < F) speeds[tid] = sh.speeds[slab * F + tid];
+  if (tid == 0) {
+    for (int i = 0; i < stages; ++i) {
+      mbar_init(&full[i], 64);  // every lane of the reader, once for what it wrote and once for its copies
+      mbar_init(&empty[i], EM_WRITERS);
+    }
+    fence_mbar_init();
   }
   pdl_trigger();
   const int b = evict_sequence(p, blockIdx.z);  // its barriers are the speeds' too
   const EvictPlan e = evict_plan(p, b);
-  const int32_t *table = p.kv.page_table + (size_t)b * mp, *dst_table = p.dst_table + (size_t)b * mp;
   const size_t row = ((size_t)b * Hkv + kvh) * mp * PAGE;
   const int32_t* kept = p.kept_idx + row;
+  // an entry's F angles: the first four speeds of every lane of a row side by side, then the other four
+  auto enter = [&](float* entry, int f, int back) {
+    const float2 a = turn_back((uint32_t)back, speeds[f]);
+    const int at = (f >> 2 & 1) * (F / 2) + (f >> 3) * 4 + (f & 3);
+    entry[at] = a.x;
+    entry[F + at] = a.y;
+  };
+  if (rope)
+    for (int i = tid; i < 64 * F; i += EM_THREADS) enter(near + i / F * 2 * F, i % F, i / F);
+  __syncthreads();
   pdl_wait();
-  if (blockIdx.x == 2 * slabs) {
+  const int chunks = (e.k + rows - 1) / rows;
+  const int pieces = bytes / 16, half = keys ? pieces / 2 : pieces;  // of a row's slab; those of its first half
+  const int shift = 31 - __clz(pieces);
+  bool alive = true;
+  auto wait = [&](uint64_t* bar, uint32_t parity) { alive = alive && __all_sync(0xffffffffu, mbar_wait(bar, parity, p.status)); };
+
+  if (warp >= EM_WRITERS) {  // ---- requests ----
+    const int32_t *table = p.kv.page_table + (size_t)b * mp, *dst_table = p.dst_table + (size_t)b * mp;
+    unsigned char* pool = static_cast<unsigned char*>(keys ? p.kv.k_pool : p.kv.v_pool);
+    const int first = slab * half * 16;
+    int next[4];  // kept tokens of this lane's rows
+    auto look = [&](int c) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int j = c * rows + x * 32 + lane;
+        next[x] = x < slabs && j < e.k ? kept[j] : -1;
+      }
+    };
+    // No more readers than stages: a reader that waits for chunk c - stages to leave has seen chunk c - readers - stages leave, so
+    // the phase before the one it waits for is over (the parity of a phase does not tell it from the one after the next).
+    const int readers = min(EM_READERS, stages);
+    int c = warp - EM_WRITERS;
+    if (c >= readers) return;
+    look(c);
 #pragma unroll 1
-    for (int j0 = 0; j0 < e.k; j0 += U * threads) {
-      float w[U];
+    for (; c < chunks; c += readers) {
+      const int st = c % stages;
+      const Stage s = stage(st);
+      unsigned char *src[4], *dst[4];
+      int low = 0x7fffffff, top = 0, back[4];
 #pragma unroll
-      for (int x = 0; x < U; ++x) {
-        const int j = j0 + x * threads + tid;
-        w[x] = j < e.k ? p.weights[row + kept[j]] : 0.f;
+      for (int x = 0; x < 4; ++x) {
+        const int i = next[x], j = c * rows + x * 32 + lane;
+        src[x] = dst[x] = nullptr;
+        back[x] = 0;
+        if (i < 0) continue;
+        const int from = table[i / PAGE], to = dst_table[j / PAGE];
+        back[x] = i - j;
+        low = min(low, back[x] >> 6);
+        top = max(top, back[x] >> 6);
+        if ((unsigned)from >= (unsigned)p.kv.num_pages || (unsigned)to >= (unsigned)p.kv.num_pages) {
+          atomicOr(p.status + ST_ERR, ERR_BAD_PAGE);
+          continue;
+        }
+        src[x] = pool + (((size_t)from * Hkv + kvh) * PAGE + i % PAGE) * ROW + first;
+        dst[x] = pool + (((size_t)to * Hkv + kvh) * PAGE + j % PAGE) * ROW + first;
+        if (src[x] == dst[x]) src[x] = dst[x] = nullptr;  // it stays where it is
       }
-      __syncthreads();
+      look(c + readers);
+      if (c >= stages) wait(&empty[st], (c / stages - 1) & 1);
+      if (!alive) break;
 #pragma unroll
-      for (int x = 0; x < U; ++x) {
-        const int j = j0 + x * threads + tid;
-        if (j < e.k) p.dst_weights[row + j] = w[x];
+      for (int x = 0; x < 4; ++x) {
+        if (x >= slabs) break;
+        s.src[x * 32 + lane] = src[x];
+        s.dst[x * 32 + lane] = dst[x];
+        s.back[x * 32 + lane] = back[x];
       }
+      __syncwarp();
+      const uint32_t data = smem_u32(s.data);
+#pragma unroll 8
+      for (int t = lane; t < CHUNK / 16; t += 32) {
+        const int r = t >> shift, q = t - (r << shift);
+        const unsigned char* from = s.src[r];
+        if (from) em_copy16(data + t * 16, from + (q < half ? q * 16 : ROW / 2 + (q - half) * 16));
+      }
+      if (rope) {
+        low = __reduce_min_sync(0xffffffffu, low);
+        top = __reduce_max_sync(0xffffffffu, top);
+        const bool fits = top - low < EM_FAR;
+        if (fits)
+          for (int m = low; m <= top; ++m)
+            for (int f = lane; f < F; f += 32) enter(s.far + (m - low) * 2 * F, f, m * 64);
+        if (lane == 0) far0[st] = fits ? low : -1;
+      }
+      asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&full[st])) : "memory");
+      mbar_arrive(&full[st]);
     }
-    if (kvh == 0 && tid == 0) p.dst_lens[b] = e.k;
+    asm volatile("cp.async.wait_all;" ::: "memory");  // also where a wait gave up: nothing is in flight when the CTA ends
     return;
   }
-  uint4* pool = static_cast<uint4*>(keys ? p.kv.k_pool : p.kv.v_pool);
-  const int lanes = PPR / slabs, half = lanes / 2, lane = tid % lanes, slab = keys ? blockIdx.x : blockIdx.x - slabs;
-  const bool high = lane >= half;
-  const int c = keys ? slab * half + (high ? lane - half + PPR / 2 : lane) : slab * lanes + lane;
-  uint2 speed[4] = {};
-  if (rope) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) speed[i] = speeds[(c % (PPR / 2)) * 8 + (high ? 4 : 0) + i];
-  }
-  auto at = [&](const int32_t* t, int slot) -> uint4* {
-    const int page = t[slot / PAGE];
-    if ((unsigned)page >= (unsigned)p.kv.num_pages) {
-      atomicOr(p.status + ST_ERR, ERR_BAD_PAGE);
-      return nullptr;
-    }
-    return pool + (((size_t)page * Hkv + kvh) * PAGE + slot % PAGE) * PPR + c;
-  };
-  const int step = threads / lanes, mine = tid / lanes;  // rows that the CTA takes side by side
-  int next[U];
-#pragma unroll
-  for (int x = 0; x < U; ++x) next[x] = mine + x * step < e.k ? kept[mine + x * step] : -1;
+
+  // ---- a warp writes every eighth chunk, and sees the others arrive ----
 #pragma unroll 1
-  for (int j0 = mine; j0 - mine < e.k; j0 += U * step) {  // the same number of turns for every thread
-    uint4 v[U];
-    uint4* dst[U];
-    int from[U];
+  for (int c = 0; c < chunks; ++c) {
+    const int st = c % stages;
+    wait(&full[st], (c / stages) & 1);
+    if (!alive) break;
+    if (c % EM_WRITERS == warp) {
+      const Stage s = stage(st);
+      const uint4* data = reinterpret_cast<const uint4*>(s.data);
+      if (!rope) {
+#pragma unroll 4
+        for (int t = lane; t < CHUNK / 16; t += 32) {
+          const int r = t >> shift, q = t - (r << shift);
+          unsigned char* to = s.dst[r];
+          if (to) *reinterpret_cast<uint4*>(to + (q < half ? q * 16 : ROW / 2 + (q - half) * 16)) = data[t];
+        }
+      } else {
+        const int f0 = lane % half, low = far0[st];
+#pragma unroll 2
+        for (int r = lane / half; r < rows; r += 32 / half) {
+          uint4* dst = reinterpret_cast<uint4*>(s.dst[r]);
+          if (dst == nullptr) continue;
+          const int back = s.back[r];
+          const uint4 lo = data[r * pieces + f0], hi = data[r * pieces + half + f0];
+          const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, h[4] = {hi.x, hi.y, hi.z, hi.w};
+          uint32_t new_l[4], new_h[4];
+          const float *a = near + (back & 63) * 2 * F + f0 * 4, *w = s.far + ((back >> 6) - max(low, 0)) * 2 * F + f0 * 4;
 #pragma unroll
-    for (int x = 0; x < U; ++x) {
-      from[x] = next[x];
-      dst[x] = nullptr;
-      v[x] = make_uint4(0u, 0u, 0u, 0u);
-      if (from[x] >= 0) {
-        const uint4* src = at(table, from[x]);
-        uint4* to = at(dst_table, j0 + x * step);
-        if (src && to && src != to) {
-          v[x] = *src;
-          dst[x] = to;
+          for (int q = 0; q < 2; ++q) {  // four pairs at a time
+            float cs[4], sn[4];
+            if (low >= 0) {
+              const float4 ac = *reinterpret_cast<const float4*>(a + q * F / 2), as = *reinterpret_cast<const float4*>(a + F + q * F / 2);
+              const float4 wc = *reinterpret_cast<const float4*>(w + q * F / 2), ws = *reinterpret_cast<const float4*>(w + F + q * F / 2);
+              cs[0] = wc.x * ac.x - ws.x * as.x; sn[0] = ws.x * ac.x + wc.x * as.x;
+              cs[1] = wc.y * ac.y - ws.y * as.y; sn[1] = ws.y * ac.y + wc.y * as.y;
+              cs[2] = wc.z * ac.z - ws.z * as.z; sn[2] = ws.z * ac.z + wc.z * as.z;
+              cs[3] = wc.w * ac.w - ws.w * as.w; sn[3] = ws.w * ac.w + wc.w * as.w;
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float2 t = turn_back((uint32_t)back, speeds[f0 * 8 + q * 4 + i]);
+                cs[i] = t.x;
+                sn[i] = t.y;
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const float l0 = bf16_lo(l[2 * q + i]), l1 = bf16_hi(l[2 * q + i]), h0 = bf16_lo(h[2 * q + i]), h1 = bf16_hi(h[2 * q + i]);
+              new_l[2 * q + i] = em_pack(l0 * cs[2 * i] - h0 * sn[2 * i], l1 * cs[2 * i + 1] - h1 * sn[2 * i + 1]);
+              new_h[2 * q + i] = em_pack(h0 * cs[2 * i] + l0 * sn[2 * i], h1 * cs[2 * i + 1] + l1 * sn[2 * i + 1]);
+            }
+          }
+          dst[f0] = back ? make_uint4(new_l[0], new_l[1], new_l[2], new_l[3]) : lo;
+          dst[f0 + ROW / 32] = back ? make_uint4(new_h[0], new_h[1], new_h[2], new_h[3]) : hi;
         }
       }
     }
-#pragma unroll
-    for (int x = 0; x < U; ++x) {
-      const int j = j0 + (U + x) * step;
-      next[x] = j < e.k ? kept[j] : -1;
-    }
-    if (rope) {
-#pragma unroll
-      for (int x = 0; x < U; ++x) {
-        const uint32_t back = (uint32_t)(from[x] - (j0 + x * step));
-        // the four pairs of this lane: its own elements, and the partner's
-        const uint32_t give0 = high ? v[x].x : v[x].z, give1 = high ? v[x].y : v[x].w;
-        const uint32_t got0 = __shfl_xor_sync(0xffffffffu, give0, half), got1 = __shfl_xor_sync(0xffffffffu, give1, half);
-        const uint32_t lo[2] = {high ? got0 : v[x].x, high ? got1 : v[x].y}, hi[2] = {high ? v[x].z : got0, high ? v[x].w : got1};
-        uint32_t new_lo[2], new_hi[2];
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          const float2 a = turn_back(back, speed[2 * w]), b2 = turn_back(back, speed[2 * w + 1]);
-          new_lo[w] = pack_bf16(bf16_lo(lo[w]) * a.x - bf16_lo(hi[w]) * a.y, bf16_hi(lo[w]) * b2.x - bf16_hi(hi[w]) * b2.y);
-          new_hi[w] = pack_bf16(bf16_lo(hi[w]) * a.x + bf16_lo(lo[w]) * a.y, bf16_hi(hi[w]) * b2.x + bf16_hi(lo[w]) * b2.y);
-        }
-        const uint32_t back0 = __shfl_xor_sync(0xffffffffu, high ? new_lo[0] : new_hi[0], half);
-        const uint32_t back1 = __shfl_xor_sync(0xffffffffu, high ? new_lo[1] : new_hi[1], half);
-        if (back) v[x] = high ? make_uint4(back0, back1, new_hi[0], new_hi[1]) : make_uint4(new_lo[0], new_lo[1], back0, back1);
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int x = 0; x < U; ++x)
-      if (dst[x]) *dst[x] = v[x];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&empty[st]);
   }
 }
 
 template <int HD>
 static void launch_move(const EvictArgs& a, cudaStream_t st) {
   const int Hkv = a.shape.n_kv_heads, rows = 2 * a.B * Hkv;
-  const int slabs = rows >= 4 * sm_count() ? 1 : HD / 32, ctas = rows * slabs;
-  const int threads = ctas <= sm_count() ? 1024 : ctas <= 2 * sm_count() ? 512 : 256;
-  SOL_LAUNCH("evict_move", evict_move_kernel<HD>, dim3(2 * slabs + 1, Hkv, a.B), dim3(threads), 0, st, a, slabs);
+  MoveShape sh;
+  sh.slabs = rows >= sm_count() ? HD / 64 : HD / 32;  // pieces of 64 bytes of a key; of 32 where CTAs are few
+  for (int f = 0; f < 64; ++f) sh.speeds[f] = make_uint2(0, 0);
+  if (a.shape.rope_theta > 0.f)
+    for (int f = 0; f < HD / 2; ++f) {
+      const double turns = exp2(-2.0 * f / HD * log2((double)a.shape.rope_theta)) * 0.15915494309189535;
+      const uint64_t fraction = (uint64_t)((turns - floor(turns)) * 0x1p64);
+      sh.speeds[f] = make_uint2((uint32_t)fraction, (uint32_t)(fraction >> 32));
+    }
+  const int each = em_stage_bytes(HD, sh.slabs), tables = 64 * 2 * (HD / 2 / sh.slabs) * 4;
+  const int room = (rows * sh.slabs > sm_count() ? 100 : 200) * 1024;  // two CTAs per SM where there are so many
+  sh.stages = std::min(EM_MAX_STAGES, (room - tables) / each);
+  const int smem = sh.stages * each + tables;
+  ensure_dynamic_smem(reinterpret_cast<const void*>(&evict_move_kernel<HD>), smem);
+  SOL_LAUNCH("evict_move", evict_move_kernel<HD>, dim3(2 * sh.slabs, Hkv, a.B), dim3(EM_THREADS), smem, st, a, sh);
 }
 
 void launch_evict(const EvictArgs& a, cudaStream_t st) {
