@@ -464,10 +464,14 @@ void launch_chain_merge(const ChainShape& c, const ChainParts& part, int Hq, int
 }
 
 // ---- the weights of a decode step ----------------------------------------------------------------
-constexpr int WK_TOKENS = RM_THREADS * 4;  // tokens of a unit
+constexpr int WK_V = 2;                          // four tokens at a time, so many times per thread
+constexpr int WK_TOKENS = RM_THREADS * 4 * WK_V;  // tokens of a unit
 
+// A CTA takes (sequence, kv-head, WK_TOKENS tokens) units in turn.  Its threads request logits and weights first and find the
+// heads' sums of weights (of chains that were cut: from the pieces) while those travel: one after the other, the waits for
+// memory were what the kernel consisted of (62 us for 160 MB).
 template <int HD>
-__global__ void __launch_bounds__(RM_THREADS) weight_kernel(const RowsDev p, int ctas, float decay, float* __restrict__ weights) {
+__global__ void __launch_bounds__(RM_THREADS, 4) weight_kernel(const RowsDev p, int ctas, float decay, float* __restrict__ weights) {
   __shared__ ChainPlan plan;
   __shared__ float lse[RM_ROWS];
   __shared__ int units[CHAIN_MAX_BATCH + 1];
@@ -475,18 +479,27 @@ __global__ void __launch_bounds__(RM_THREADS) weight_kernel(const RowsDev p, int
   pdl_trigger();
   chain_plan(p.c, plan, ctas, nullptr);
   const int G = p.c.G;
-  if (tid == 0) {
+  if (tid < 32) {  // units before each sequence
     int n = 0;
-    for (int b = 0; b < p.c.B; ++b) {
-      units[b] = n;
-      n += max(1, (plan.at(b).T + WK_TOKENS - 1) / WK_TOKENS) * p.c.Hkv;
+    for (int b0 = 0; b0 < CHAIN_MAX_BATCH; b0 += 32) {
+      const int b = b0 + tid;
+      int v = b < p.c.B ? max(1, (plan.at(b).T + WK_TOKENS - 1) / WK_TOKENS) * p.c.Hkv : 0;
+      const int mine = v;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, v, o);
+        if (tid >= o) v += x;
+      }
+      units[b] = n + v - mine;
+      n += __shfl_sync(0xffffffffu, v, 31);
     }
-    units[p.c.B] = n;
+    if (tid == 0) units[CHAIN_MAX_BATCH] = n;
   }
   __syncthreads();
   pdl_wait();
   const size_t stride = (size_t)p.c.kv.max_pages_per_seq * PAGE;
-  for (int u = blockIdx.x; u < units[p.c.B]; u += gridDim.x) {
+#pragma unroll 1
+  for (int u = blockIdx.x; u < units[CHAIN_MAX_BATCH]; u += gridDim.x) {
     int lo = 0, hi = p.c.B - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -494,9 +507,29 @@ __global__ void __launch_bounds__(RM_THREADS) weight_kernel(const RowsDev p, int
       else hi = mid - 1;
     }
     const int b = lo, T = plan.at(b).T, per = max(1, (T + WK_TOKENS - 1) / WK_TOKENS);
-    const int kvh = (u - units[b]) / per, chunk = (u - units[b]) - kvh * per;
+    const int kvh = (u - units[b]) / per, chunk = (u - units[b]) - kvh * per, tok0 = chunk * WK_TOKENS + tid * 4;
+    const size_t bk = (size_t)b * p.c.Hkv + kvh;
+    float* dst = weights + bk * stride;
+    float4 s[4][WK_V], w[WK_V], sum[WK_V];
+    auto request = [&](int g0) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int v = 0; v < WK_V; ++v) {
+          const int tok = tok0 + v * RM_THREADS * 4;
+          s[g][v] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+          if (g0 + g < G && tok < T) s[g][v] = *reinterpret_cast<const float4*>(p.logits + (bk * G + g0 + g) * stride + tok);
+        }
+    };
+    request(0);
+#pragma unroll
+    for (int v = 0; v < WK_V; ++v) {
+      const int tok = tok0 + v * RM_THREADS * 4;
+      sum[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+      w[v] = tok < T ? *reinterpret_cast<const float4*>(dst + tok) : sum[v];
+    }
     const ChainCut cut = chain_cut(p.c, plan, b, kvh);
-    __syncthreads();
+    __syncthreads();  // the sums of the unit before have been read
     if (cut.cut()) {
       const int g = tid >> 4;
       if (g < (G + 1) / 2 * 2) {  // whole warps
@@ -508,21 +541,31 @@ __global__ void __launch_bounds__(RM_THREADS) weight_kernel(const RowsDev p, int
       lse[tid] = p.lse[(size_t)b * p.Hq + kvh * G + tid];
     }
     __syncthreads();
-    const int tok = chunk * WK_TOKENS + tid * 4;
-    if (tok >= T) continue;
-    const size_t bk = (size_t)b * p.c.Hkv + kvh;
-    float w[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int g = 0; g < G; ++g) {
-      const float4 s = *reinterpret_cast<const float4*>(p.logits + (bk * G + g) * stride + tok);
-      w[0] += exp2f(s.x - lse[g]);
-      w[1] += exp2f(s.y - lse[g]);
-      w[2] += exp2f(s.z - lse[g]);
-      w[3] += exp2f(s.w - lse[g]);
-    }
-    float* dst = weights + bk * stride + tok;
+#pragma unroll 1
+    for (int g0 = 0; g0 < G; g0 += 4) {
+      if (g0) request(g0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (tok + i < T) dst[i] = tok + i == T - 1 ? w[i] : decay * dst[i] + w[i];
+      for (int g = 0; g < 4; ++g) {
+        const float z = g0 + g < G ? lse[g0 + g] : INFINITY;
+#pragma unroll
+        for (int v = 0; v < WK_V; ++v) {
+          sum[v].x += exp2f(s[g][v].x - z);
+          sum[v].y += exp2f(s[g][v].y - z);
+          sum[v].z += exp2f(s[g][v].z - z);
+          sum[v].w += exp2f(s[g][v].w - z);
+        }
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < WK_V; ++v) {
+      const int tok = tok0 + v * RM_THREADS * 4;
+      if (tok >= T) continue;
+      const float old[4] = {w[v].x, w[v].y, w[v].z, w[v].w}, got[4] = {sum[v].x, sum[v].y, sum[v].z, sum[v].w};
+      float now[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) now[i] = tok + i < T - 1 ? decay * old[i] + got[i] : tok + i == T - 1 ? got[i] : old[i];
+      *reinterpret_cast<float4*>(dst + tok) = make_float4(now[0], now[1], now[2], now[3]);
+    }
   }
 }
 
@@ -543,7 +586,7 @@ static void launch_rows(RowsDev d, const RowsArgs& a, cudaStream_t st) {
   d.part = chain_parts(a.part, ctas, rows, HD);
   ensure_dynamic_smem(reinterpret_cast<const void*>(&rows_attn_kernel<HD, ROWS>), Z::SMEM);
   SOL_LAUNCH("rows_attn", (rows_attn_kernel<HD, ROWS>), dim3(ctas), dim3(RA_THREADS), Z::SMEM, st, kmap, vmap, d);
-  if (a.weights) SOL_LAUNCH("attn_weights", weight_kernel<HD>, dim3(4 * ctas), dim3(RM_THREADS), 0, st, d, ctas, a.decay, a.weights);
+  if (a.weights) SOL_LAUNCH("attn_weights", weight_kernel<HD>, dim3(4 * sm_count()), dim3(RM_THREADS), 0, st, d, ctas, a.decay, a.weights);
   else launch_chain_merge(d.c, d.part, d.Hq, HD, ctas, d.out, st);
 }
 
