@@ -23,9 +23,7 @@
 namespace sol {
 
 constexpr int RA_MAX_ROWS = 16;  // query rows of a chain at most
-constexpr int RA_WARPS = 6;   // consumer warps
-constexpr int RA_DEPTH = 2;   // stages of a warp's ring
-constexpr int RA_THREADS = (RA_WARPS + 1) * 32;
+constexpr int RA_STAGES = 12;     // of all warps' rings
 constexpr int RA_MIN_TILES = 4;
 constexpr int ra_piece_cost(int hd) { return hd == 64 ? 8 : 4; }
 
@@ -50,11 +48,14 @@ struct RaSize {
   static constexpr int STEPS = PAGE / TOK;     // of a tile
   static constexpr int HALF = TOK * 128;       // a 64-wide half of the keys: [TOK tokens][128 B]
   static constexpr int TILE = HALF * (HD / 64);
-  static constexpr int STAGES = RA_WARPS * RA_DEPTH;
+  // Consumer warps, stages of a warp's ring: one warp per quarter of the SM (the producer in the fourth) keeps up and has a deep
+  // ring (128 ragged decode steps 340 us, with six warps of two stages 352; 32 chains of 8000 with 16 rows 215 and 222, four warps
+  // 227).  Only 16 rows over the short tiles of head_dim 64 keep three warps busy (16 sequences of 4000: 41 us, with six 37).
+  static constexpr int WARPS = HD == 64 && ROWS == 16 ? 6 : 3, DEPTH = RA_STAGES / WARPS, THREADS = (WARPS + 1) * 32;
   static constexpr int NB = ROWS == 16 ? 2 : 1;         // blocks of eight rows
   static constexpr int REGS = (HD / 16 * 4 + 4) * NB;   // sums, two maxima, two sums of weights
   static constexpr int MERGE = 2 * REGS * 32 * 4;
-  static constexpr int SMEM = 1024 + STAGES * 2 * TILE + MERGE;
+  static constexpr int SMEM = 1024 + RA_STAGES * 2 * TILE + MERGE;
 };
 
 // Shared-memory address of 16-byte piece c of token r of a step.
@@ -62,26 +63,27 @@ template <int HALF>
 __device__ __forceinline__ uint32_t ra_piece(uint32_t base, int r, int c) {
   return base + (uint32_t)((c >> 3) * HALF + r * 128 + (((c & 7) ^ (r & 7)) << 4));
 }
+template <int THREADS>
 __device__ __forceinline__ void ra_consumer_sync() {
   __syncwarp();
-  asm volatile("bar.sync 1, %0;" ::"n"(RA_WARPS * 32) : "memory");
+  asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
 }
 
 template <int HD, int ROWS>
-__global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_constant__ CUtensorMap kmap,
-                                                                  const __grid_constant__ CUtensorMap vmap, const RowsDev p) {
+__global__ void __launch_bounds__(RaSize<HD, ROWS>::THREADS, 1)
+    rows_attn_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const RowsDev p) {
   using Z = RaSize<HD, ROWS>;
   constexpr int KS = HD / 16, MT = Z::TOK / 16, NB = Z::NB;  // steps of head_dim, of tokens; blocks of eight rows
   constexpr bool PACK = ROWS == 4;  // rows 4 .. 7 of the block are rows 0 .. 3 again: their weights' low parts
   extern __shared__ unsigned char ra_smem[];
   __shared__ ChainPlan plan;
-  __shared__ uint64_t full[Z::STAGES], empty[Z::STAGES];
-  __shared__ int page_ok[Z::STAGES];
+  __shared__ uint64_t full[RA_STAGES], empty[RA_STAGES];
+  __shared__ int page_ok[RA_STAGES];
   unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(ra_smem) + 1023) & ~(uintptr_t)1023);
-  float* merge = reinterpret_cast<float*>(ring + Z::STAGES * 2 * Z::TILE);
+  float* merge = reinterpret_cast<float*>(ring + RA_STAGES * 2 * Z::TILE);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    for (int s = 0; s < Z::STAGES; ++s) {
+    for (int s = 0; s < RA_STAGES; ++s) {
       mbar_init(&full[s], 1);
       mbar_init(&empty[s], 1);
     }
@@ -96,7 +98,7 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
   const int u0 = range.x, u1 = range.y;
 
   if (tid == 0) chain_describe(p.c, plan, blockIdx.x, u0, u1, p.part.desc);
-  if (warp == RA_WARPS) {  // ---- the producer ----
+  if (warp == Z::WARPS) {  // ---- the producer ----
     int it = 0;
     for (int u = u0; u < u1;) {
       const ChainPiece c = chain_piece(p.c, plan, u, u1);
@@ -107,12 +109,12 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
         const int cnt = min(32, c.tile1 - g0);
         for (int x = 0; x < cnt * Z::STEPS; ++x, ++it) {
           int page = __shfl_sync(0xffffffffu, mine, x / Z::STEPS);
-          // step `it` goes to warp it % RA_WARPS, whose use number `use` of its ring it is
-          const int use = it / RA_WARPS, st = it % RA_WARPS * RA_DEPTH + use % RA_DEPTH;
-          if (use >= RA_DEPTH && !__all_sync(0xffffffffu, mbar_wait(&empty[st], (use / RA_DEPTH - 1) & 1, p.status))) {
+          // step `it` goes to warp it % Z::WARPS, whose use number `use` of its ring it is
+          const int use = it / Z::WARPS, st = it % Z::WARPS * Z::DEPTH + use % Z::DEPTH;
+          if (use >= Z::DEPTH && !__all_sync(0xffffffffu, mbar_wait(&empty[st], (use / Z::DEPTH - 1) & 1, p.status))) {
             // the consumers give up too; what has been requested still arrives before the CTA ends
-            for (int i = max(0, it - Z::STAGES); i < it; ++i)
-              mbar_wait(&full[i % RA_WARPS * RA_DEPTH + i / RA_WARPS % RA_DEPTH], (i / RA_WARPS / RA_DEPTH) & 1, p.status);
+            for (int i = max(0, it - RA_STAGES); i < it; ++i)
+              mbar_wait(&full[i % Z::WARPS * Z::DEPTH + i / Z::WARPS % Z::DEPTH], (i / Z::WARPS / Z::DEPTH) & 1, p.status);
             return;
           }
           if (lane == 0) {
@@ -180,10 +182,10 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
 
     const int len = (c.tile1 - c.tile0) * Z::STEPS;
 #pragma unroll 1
-    for (int x = (warp - it % RA_WARPS + RA_WARPS) % RA_WARPS; x < len; x += RA_WARPS) {
-      const int use = (it + x) / RA_WARPS, st = warp * RA_DEPTH + use % RA_DEPTH;
+    for (int x = (warp - it % Z::WARPS + Z::WARPS) % Z::WARPS; x < len; x += Z::WARPS) {
+      const int use = (it + x) / Z::WARPS, st = warp * Z::DEPTH + use % Z::DEPTH;
       const int tok0 = c.tile0 * PAGE + x * Z::TOK;  // first token of the step
-      alive = alive && __all_sync(0xffffffffu, mbar_wait(&full[st], (use / RA_DEPTH) & 1, p.status));
+      alive = alive && __all_sync(0xffffffffu, mbar_wait(&full[st], (use / Z::DEPTH) & 1, p.status));
       if (!alive) break;
       const uint32_t kb = smem_u32(ring + (size_t)st * 2 * Z::TILE), vb = kb + Z::TILE;
       const bool ok = page_ok[st] != 0;
@@ -345,11 +347,11 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
     }
     it += len;
 
-    // ---- merge the warps, 4 and 5 into 0 and 1, then 2 and 3, then 1; a lane holds the same elements in every warp ----
+    // ---- merge the warps (six: 4 and 5 into 0 and 1), then 2 and 3, then 1; a lane holds the same elements in every warp ----
 #pragma unroll 1
-    for (int half = 4; half; half >>= 1) {
+    for (int half = Z::WARPS > 4 ? 4 : 2; half; half >>= 1) {
       float* slot = merge + (size_t)(warp & 1 & (half - 1)) * Z::REGS * 32 + lane;
-      const bool gives = warp >= half && warp < min(2 * half, RA_WARPS), takes = warp + half < min(2 * half, RA_WARPS);
+      const bool gives = warp >= half && warp < min(2 * half, Z::WARPS), takes = warp + half < min(2 * half, Z::WARPS);
       if (gives) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -365,7 +367,7 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
           }
         }
       }
-      ra_consumer_sync();
+      ra_consumer_sync<Z::WARPS * 32>();
       if (takes) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -385,7 +387,7 @@ __global__ void __launch_bounds__(RA_THREADS, 1) rows_attn_kernel(const __grid_c
             for (int e = 0; e < 4; ++e) o[nb][k][e] = o[nb][k][e] * f[e & 1] + s[(k * 4 + e) * 32] * h[e & 1];
         }
       }
-      ra_consumer_sync();
+      ra_consumer_sync<Z::WARPS * 32>();
     }
     if (warp == 0) {
       const bool whole = c.whole();
@@ -471,7 +473,7 @@ constexpr int WK_TOKENS = RM_THREADS * 4 * WK_V;  // tokens of a unit
 // heads' sums of weights (of chains that were cut: from the pieces) while those travel: one after the other, the waits for
 // memory were what the kernel consisted of (62 us for 160 MB).
 template <int HD>
-__global__ void __launch_bounds__(RM_THREADS, 4) weight_kernel(const RowsDev p, int ctas, float decay, float* __restrict__ weights) {
+__global__ void __launch_bounds__(RM_THREADS, 3) weight_kernel(const RowsDev p, int ctas, float decay, float* __restrict__ weights) {
   __shared__ ChainPlan plan;
   __shared__ float lse[RM_ROWS];
   __shared__ int units[CHAIN_MAX_BATCH + 1];
@@ -585,8 +587,8 @@ static void launch_rows(RowsDev d, const RowsArgs& a, cudaStream_t st) {
   const int ctas = (int)std::min<size_t>(sm_count(), a.part_bytes / chain_part_bytes(1, rows, HD));
   d.part = chain_parts(a.part, ctas, rows, HD);
   ensure_dynamic_smem(reinterpret_cast<const void*>(&rows_attn_kernel<HD, ROWS>), Z::SMEM);
-  SOL_LAUNCH("rows_attn", (rows_attn_kernel<HD, ROWS>), dim3(ctas), dim3(RA_THREADS), Z::SMEM, st, kmap, vmap, d);
-  if (a.weights) SOL_LAUNCH("attn_weights", weight_kernel<HD>, dim3(4 * sm_count()), dim3(RM_THREADS), 0, st, d, ctas, a.decay, a.weights);
+  SOL_LAUNCH("rows_attn", (rows_attn_kernel<HD, ROWS>), dim3(ctas), dim3(Z::THREADS), Z::SMEM, st, kmap, vmap, d);
+  if (a.weights) SOL_LAUNCH("attn_weights", weight_kernel<HD>, dim3(3 * sm_count()), dim3(RM_THREADS), 0, st, d, ctas, a.decay, a.weights);
   else launch_chain_merge(d.c, d.part, d.Hq, HD, ctas, d.out, st);
 }
 
