@@ -85,6 +85,18 @@ __device__ __forceinline__ bool mbar_try_wait_at(uint32_t bar_smem, uint32_t par
   return ok != 0;
 }
 __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) { return mbar_try_wait_at(smem_u32(bar), parity); }
+// The same question without the hardware's nap: a warp that sleeps in try_wait takes some hundred cycles to wake.
+__device__ __forceinline__ bool mbar_test_wait_at(uint32_t bar_smem, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar_smem), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 // Bounded wait: gives up after `limit` polls, raises ERR_TIMEOUT in the status
 // words and returns false; the caller then skips its work and leaves.
 constexpr uint32_t WAIT_LIMIT = 1u << 20;

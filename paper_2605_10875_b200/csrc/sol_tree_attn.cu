@@ -35,6 +35,7 @@ constexpr int TA_TILE = 2 * PAGE;       // tokens of a tile
 constexpr int TA_MIN_TILES = 2;
 constexpr int ta_piece_cost(int hd) { return hd == 64 ? 8 : 4; }
 constexpr int TA_THREADS = 12 * 32;
+constexpr uint32_t POLL_LIMIT = 1u << 24;  // polls of the products' warp: some tenths of a second
 constexpr float TA_SLACK = 8.f;         // weights reach 2^8 before the maximum moves
 constexpr int TA_EX = 32;               // columns handed over at a time at the end of a piece
 enum : int { TAW_KEYS = 8, TAW_VALUES = 9, TAW_MMA = 10, TAW_CLEAR = 11 };
@@ -73,7 +74,7 @@ struct TreeShared {
   ChainPlan plan;
   uint64_t k_full[TaSize<HD>::K_SLOTS], k_empty[TaSize<HD>::K_SLOTS];
   uint64_t v_full[TaSize<HD>::V_SLOTS], v_empty[TaSize<HD>::V_SLOTS], v_clean[TaSize<HD>::V_SLOTS];
-  uint64_t q_ready, s_full[2], p_ready[2], o_end[2];
+  uint64_t q_ready, s_full[2], p_half[2], p_ready[2], o_end[2];
   TreeClearJob jobs[TA_JOBS];
   unsigned long long dirty[TA_JOBS];  // per job: drafted tokens whose values were taken out
   int posted;                         // jobs so far
@@ -257,7 +258,8 @@ __device__ void tree_clear(const TreeDev& p, TreeShared<HD>& sh, uint32_t v_ring
 }
 
 // ---- tensor cores ----
-// This warp's pace is the kernel's.  It waits for all that a turn needs at once, a barrier per lane, and issues a turn's products
+// This warp's pace is the kernel's.  It waits without naps (mbar_test_wait_at) for all that a step needs at once, a barrier per
+// lane, and issues a step's products
 // and commits in one elected block on operands that are the same in all lanes: 32 to 62 cycles a product, where predicated ones
 // took 80 and blocks on lanes' own values more than that.
 template <int HD>
@@ -268,15 +270,15 @@ __device__ void tree_mma(const TreeDev& p, TreeShared<HD>& sh, uint32_t q_oper, 
   const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
   const uint64_t q_desc = umma_smem_desc(q_oper, 16, 1024);
   const uint64_t k_desc = umma_smem_desc(k_ring, 16, 1024), v_desc = umma_smem_desc(v_ring, Z::CHUNK, 1024);
-  const uint32_t k_full = smem_u32(sh.k_full), v_full = smem_u32(sh.v_full), v_clean = smem_u32(sh.v_clean), p_ready = smem_u32(sh.p_ready);
+  const uint32_t k_full = smem_u32(sh.k_full), v_full = smem_u32(sh.v_full), v_clean = smem_u32(sh.v_clean), p_half = smem_u32(sh.p_half), p_ready = smem_u32(sh.p_ready);
   bool alive = true;
   auto wait = [&](uint32_t bar, uint32_t parity) {  // bar, parity: this lane's.  After one that gave up, the others return at once
-    if (__all_sync(0xffffffffu, mbar_try_wait_at(bar, parity)) || !alive) return;
-    bool ok = false;
+    if (!alive) return;
 #pragma unroll 1
-    for (uint32_t i = 0; i < WAIT_LIMIT && !ok; ++i) ok = mbar_try_wait_at(bar, parity);
-    alive = __all_sync(0xffffffffu, ok);
-    if (!ok) atomicOr(p.status + ST_ERR, ERR_TIMEOUT);
+    for (uint32_t i = 0; i < POLL_LIMIT; ++i)
+      if (__all_sync(0xffffffffu, mbar_test_wait_at(bar, parity))) return;
+    alive = false;
+    if (lane == 0) atomicOr(p.status + ST_ERR, ERR_TIMEOUT);
   };
   int k_slot = 0, v_slot = 0;  // of the next tiles
   uint32_t k_phase = 0, v_phase = 0, clean_phases = 0, p_phases = 0;  // clean_phases, p_phases: a bit per slot, per unit
@@ -303,13 +305,15 @@ __device__ void tree_mma(const TreeDev& p, TreeShared<HD>& sh, uint32_t q_oper, 
     umma_commit(&sh.s_full[unit]);
     if (last) umma_commit(&sh.k_empty[k_slot]);
   };
-  // ... and the product of the unit's weights with the values
-  auto values = [&](int unit, bool fresh, bool last, bool end) {
+  // ... and the product of the unit's weights with the values: of the tile's first half, of its second
+  auto values = [&](int unit, int half, bool fresh) {
     const uint32_t base = tmem + unit * Z::UNIT;
     const uint64_t b = v_desc + (uint64_t)(v_slot * (Z::OPER >> 4));
 #pragma unroll
-    for (int k = 0; k < TA_TILE / 16; ++k)
+    for (int k = half * 4; k < half * 4 + 4; ++k)
       umma_bf16_ts(base + TA_TILE, base + k * 8, b + (uint64_t)(k * 2048 >> 4), O_IDESC, !fresh || k > 0);
+  };
+  auto values_end = [&](int unit, bool last, bool end) {
     if (last) umma_commit(&sh.v_empty[v_slot]);
     if (end) {
       umma_commit(&sh.o_end[unit]);
@@ -321,14 +325,25 @@ __device__ void tree_mma(const TreeDev& p, TreeShared<HD>& sh, uint32_t q_oper, 
     const TreePiece c = tree_piece(p.c, sh.plan, u, u1);
     const int steps = c.steps, mixed = c.first_mixed() - c.tile0;
     wait(smem_u32(&sh.q_ready), piece & 1);
-    // a turn's barriers: the unit's weights, the next keys, the values (cleared, where that is needed)
-    auto turn = [&](int unit, int j, bool keys) {
+    // A unit's turn, as its weights come, half a tile at a time: their product with the values (cleared, where that is needed),
+    // then, if there are `keys`, the next scores
+    auto turn = [&](int unit, int j, bool fresh, bool last, bool keys, uint64_t queries) {
       const bool mix = j >= mixed;
-      const uint32_t bar = lane == 0 ? p_ready + unit * 8 : lane == 1 && keys ? k_full + k_slot * 8 : (mix ? v_clean : v_full) + v_slot * 8;
-      const uint32_t parity = lane == 0 ? (p_phases >> unit) & 1 : lane == 1 && keys ? k_phase : mix ? (clean_phases >> v_slot) & 1 : v_phase;
-      wait(bar, parity);
+      const uint32_t mine = (p_phases >> unit) & 1;
+      wait(lane == 0 ? p_half + unit * 8 : (mix ? v_clean : v_full) + v_slot * 8,
+           lane == 0 ? mine : mix ? (clean_phases >> v_slot) & 1 : v_phase);
+      tc_fence_after();
+      if (elect_one()) values(unit, 0, fresh);
+      __syncwarp();
+      wait(lane == 0 || !keys ? p_ready + unit * 8 : k_full + k_slot * 8, lane == 0 || !keys ? mine : k_phase);
       p_phases ^= 1u << unit;
       tc_fence_after();
+      if (elect_one()) {
+        values(unit, 1, false);
+        values_end(unit, last, !keys);
+        if (keys) scores(unit, queries, last);
+      }
+      __syncwarp();
     };
     auto values_used = [&](int j) {
       if (j >= mixed) clean_phases ^= 1u << v_slot;
@@ -347,20 +362,8 @@ __device__ void tree_mma(const TreeDev& p, TreeShared<HD>& sh, uint32_t q_oper, 
 #pragma unroll 1
       for (int j = 0; j < steps; ++j) {
         const bool more = j + 1 < steps;
-        turn(0, j, more);
-        if (elect_one()) {
-          values(0, j == 0, false, !more);
-          if (more) scores(0, q_desc, false);
-        }
-        __syncwarp();
-        wait(p_ready + 8, (p_phases >> 1) & 1);
-        p_phases ^= 2u;
-        tc_fence_after();
-        if (elect_one()) {
-          values(1, j == 0, true, !more);
-          if (more) scores(1, q1_desc, true);
-        }
-        __syncwarp();
+        turn(0, j, j == 0, false, more, q_desc);
+        turn(1, j, j == 0, true, more, q1_desc);
         values_used(j);
         if (more) k_step();
       }
@@ -374,14 +377,8 @@ __device__ void tree_mma(const TreeDev& p, TreeShared<HD>& sh, uint32_t q_oper, 
       }
 #pragma unroll 1
       for (int j = 0; j < steps; ++j) {
-        const int unit = j & 1;
         const bool more = j + 2 < steps;
-        turn(unit, j, more);
-        if (elect_one()) {
-          values(unit, j < 2, true, !more);
-          if (more) scores(unit, q_desc, true);
-        }
-        __syncwarp();
+        turn(j & 1, j, j < 2, true, more, q_desc);
         values_used(j);
         if (more) k_step();
       }
@@ -420,10 +417,12 @@ __device__ __noinline__ void tree_rescale(uint32_t tm_o, float f) {
 
 // A tile's W tokens from column `seg` W of the scores on: weights to the front of the scores' columns (the other tokens' are zero).
 // base: the first of these tokens; m, l: running maximum (base 2) and sum; fresh: the unit has no sums yet.  (Its products so far
-// are over: these scores were asked for after them.)
+// are over: these scores were asked for after them.)  A whole tile's weights are handed over in two halves: the first is multiplied
+// while the second is computed (256 rows of the 8B shape 295 -> 280 us, 48 ragged sequences 169 -> 151).  A quarter of the powers as
+// a cubic on the FMA pipes instead of the special-function unit was slower (289 -> 299, 151 -> 177).
 template <int HD, int W>
 __device__ __forceinline__ void tree_step(const TreeDev& p, uint32_t tm_s, int seg, int base, int C, uint64_t nodes, int there,
-                                          bool fresh, float& m, float& l) {
+                                          bool fresh, float& m, float& l, uint64_t* first_half) {
   uint32_t s[W];
 #pragma unroll
   for (int x = 0; x < W; x += 32) tmem_ld32_issue(tm_s + seg * W + x, s + x);
@@ -459,6 +458,12 @@ __device__ __forceinline__ void tree_step(const TreeDev& p, uint32_t tm_s, int s
     sum[i & 1] = ta_add2(sum[i & 1], f32x2(a, b));
     w[i] = ta_pack(a, b);
     if (W == TA_TILE && i == 31) tmem_st32(tm_s, w);
+    if (W == TA_TILE && i == 35) {  // stored by now
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (threadIdx.x % 32 == 0) mbar_arrive(first_half);
+    }
   }
   if constexpr (W == TA_TILE) {
     tmem_st32(tm_s + 32, w + 32);
@@ -571,13 +576,16 @@ __device__ void tree_softmax(const TreeDev& p, TreeShared<HD>& sh, unsigned char
       wait(&sh.s_full[unit], done & 1);
       tc_fence_after();
       if (warp_real) {
-        if (c.lanes == 128) tree_step<HD, 128>(p, tm_s, 0, base, c.C, nodes, there, j == from, m, l);
-        else if (c.lanes == 64) tree_step<HD, 64>(p, tm_s, seg, base + seg * 64, c.C, nodes, there, j == from, m, l);
-        else tree_step<HD, 32>(p, tm_s, seg, base + seg * 32, c.C, nodes, there, j == from, m, l);
+        if (c.lanes == 128) tree_step<HD, 128>(p, tm_s, 0, base, c.C, nodes, there, j == from, m, l, &sh.p_half[unit]);
+        else if (c.lanes == 64) tree_step<HD, 64>(p, tm_s, seg, base + seg * 64, c.C, nodes, there, j == from, m, l, &sh.p_half[unit]);
+        else tree_step<HD, 32>(p, tm_s, seg, base + seg * 32, c.C, nodes, there, j == from, m, l, &sh.p_half[unit]);
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.p_ready[unit]);
+      if (lane == 0) {
+        if (!warp_real || c.lanes < TA_TILE) mbar_arrive(&sh.p_half[unit]);
+        mbar_arrive(&sh.p_ready[unit]);
+      }
     }
     const int u_next = c.next;
     TreePiece next = c;
@@ -681,6 +689,7 @@ __global__ void __launch_bounds__(TA_THREADS, 1) tree_attn_kernel(const __grid_c
     mbar_init(&sh.q_ready, 256);
     for (int x = 0; x < 2; ++x) {
       mbar_init(&sh.s_full[x], 1);
+      mbar_init(&sh.p_half[x], 4);
       mbar_init(&sh.p_ready[x], 4);
       mbar_init(&sh.o_end[x], 2);
     }
