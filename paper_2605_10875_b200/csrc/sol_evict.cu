@@ -165,30 +165,34 @@ __device__ __forceinline__ float2 turn_back(uint32_t back, uint2 speed) {
                      __uint_as_float(__float_as_uint(sin_) ^ (quarter & 0x80000000u)));
 }
 
-// A CTA moves `1 / slabs` of every kept row of a (sequence, kv-head)'s keys or values, chunks of 32 slabs rows through a ring in
-// shared memory: up to eight warps request chunks in turn, 16 bytes a lane, eight write them out in turn.  In place this is safe: row j
-// goes to slot j and kept_idx[j] >= j, so what the write of a chunk covers is a row of that chunk or an earlier one, and a warp
-// writes a chunk only after it has seen that chunk and all before it arrive; what is requested later lies behind every slot
-// written so far; and no other CTA touches these pieces.
+// A CTA moves `1 / slabs` of every kept row of a (sequence, kv-head)'s keys or values, chunks of 32 rows through a ring in shared
+// memory: half of its warps request chunks in turn, 16 bytes a lane, half write them out in turn, and one says how many have
+// arrived.  In place this is safe: row j goes to slot j and kept_idx[j] >= j, so what the write of a chunk covers is a row of that
+// chunk or an earlier one, and a warp writes a chunk only when that chunk and all before it have arrived; what is requested later
+// lies behind every slot written so far; and no other CTA touches these pieces.
 // Keys: a slab of a row is a piece of its first half and the piece that is rotated with it, eight pairs per lane.  How far a row
 // moves back never falls from one row to the next and hardly changes within a chunk, so its angle is put together from two tables
 // in shared memory, of 0 .. 63 positions and of the chunk's few multiples of 64 (an angle from the polynomials for every pair takes
 // three times the instructions); chunks that span more have their angles from the polynomials.
-// Bound by HBM for batches, by the latency of a chunk times the chunks of the longest sequence otherwise.  (Rows read into
-// registers, between barriers, took 4 us a round, 317 us for half of 24 ragged caches; bulk copies of single rows 25 to 40 ns
-// each, 1447 us.)
-constexpr int EM_READERS = 8, EM_WRITERS = 8;  // warps
-constexpr int EM_THREADS = (EM_READERS + EM_WRITERS) * 32;
+// Bound by HBM and the writers' instructions for batches (half of 24 ragged caches, 1.1 GB: 221 us), by the time of a chunk times
+// the chunks of the longest sequence otherwise (half of 30000 tokens: 87 us).  Dropped: rows read into registers, between barriers,
+// 4 us a round, 317 us for the first; bulk copies of single rows, 25 to 40 ns each, 1447 us; every writer asking for every chunk
+// itself, 250 ns a chunk, 33 us where it is now 26; seven readers for a CTA that has an SM to itself, 121 us for the second.
+constexpr int EM_FEW = 7, EM_MANY = 15;  // warps that read: where two CTAs share an SM, where one has it to itself
+constexpr uint32_t EM_POLLS = 1u << 22;  // some tenths of a second
 constexpr int EM_FAR = 4;          // multiples of 64 positions in a chunk's table
-constexpr int EM_MAX_STAGES = 24;
+constexpr int EM_MAX_STAGES = 30;  // a warp's lanes ask for as many at once
 
 struct MoveShape {
-  int slabs, stages;
+  int slabs, key_stages, value_stages;
   uint2 speeds[64];  // turns per position of a head's pairs, as 64-bit fractions: low, high word
 };
-// Shared memory of a stage: the rows, where each comes from, goes to and how far it moves, angles of EM_FAR multiples of 64.
+// Shared memory of a stage: the rows, where each comes from, goes to and how far it moves; keys: angles of EM_FAR multiples of 64.
 __host__ __device__ constexpr int em_far_bytes(int hd, int slabs) { return EM_FAR * 2 * (hd / 2 / slabs) * 4; }
-__host__ __device__ constexpr int em_stage_bytes(int hd, int slabs) { return 32 * hd * 2 + 32 * slabs * (8 + 8 + 4) + em_far_bytes(hd, slabs); }
+__host__ __device__ constexpr int em_stage_bytes(int hd, int slabs, bool keys) {
+  return 32 * (hd * 2 / slabs + 8 + 8 + 4) + (keys ? em_far_bytes(hd, slabs) : 0);
+}
+__host__ __device__ constexpr int em_near_bytes(int hd, int slabs) { return 64 * 2 * (hd / 2 / slabs) * 4; }
 
 __device__ __forceinline__ void em_copy16(uint32_t dst_smem, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst_smem), "l"(src) : "memory");
@@ -200,22 +204,24 @@ __device__ __forceinline__ uint32_t em_pack(float lo, float hi) {
   return y;
 }
 
-template <int HD>
-__global__ void __launch_bounds__(EM_THREADS) evict_move_kernel(const EvictArgs p, const MoveShape sh) {
+template <int HD, int READERS>
+__global__ void __launch_bounds__((2 * READERS + 2) * 32) evict_move_kernel(const EvictArgs p, const MoveShape sh) {
+  constexpr int WRITERS = READERS + 1, ORDER = WRITERS + READERS, THREADS = (ORDER + 1) * 32;
   constexpr int ROW = HD * 2;      // bytes of a row
-  constexpr int CHUNK = 32 * ROW;  // bytes of a chunk: 32 slabs rows of ROW / slabs bytes
   extern __shared__ __align__(128) unsigned char em_smem[];
   __shared__ uint64_t full[EM_MAX_STAGES], empty[EM_MAX_STAGES];
+  __shared__ int arrived;            // chunks from the first on, without a gap
   __shared__ uint2 speeds[HD / 2];   // of the slab
   __shared__ int far0[EM_MAX_STAGES];  // first multiple of 64 in the stage's table; -1: its angles are in no table
-  const int slabs = sh.slabs, stages = sh.stages, rows = 32 * slabs, bytes = ROW / slabs, F = HD / 2 / slabs;
+  const int slabs = sh.slabs, bytes = ROW / slabs, F = HD / 2 / slabs, chunk = 32 * bytes;
   const int kvh = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int Hkv = p.shape.n_kv_heads, mp = p.kv.max_pages_per_seq;
   const bool keys = blockIdx.x < slabs, rope = keys && p.shape.rope_theta > 0.f;
+  const int stages = keys ? sh.key_stages : sh.value_stages;
   const int slab = keys ? blockIdx.x : blockIdx.x - slabs;
   float* near = reinterpret_cast<float*>(em_smem);  // [64][2][F] cosines, sines
-  unsigned char* stage0 = em_smem + 64 * 2 * F * 4;
-  const int stage_bytes = em_stage_bytes(HD, slabs);
+  unsigned char* stage0 = em_smem + (keys ? em_near_bytes(HD, slabs) : 0);
+  const int stage_bytes = em_stage_bytes(HD, slabs, keys);
   struct Stage {
     unsigned char* data;
     unsigned char **src, **dst;  // nullptr: nothing to move
@@ -225,18 +231,19 @@ __global__ void __launch_bounds__(EM_THREADS) evict_move_kernel(const EvictArgs 
   auto stage = [&](int st) {
     Stage s;
     s.data = stage0 + (size_t)st * stage_bytes;
-    s.far = reinterpret_cast<float*>(s.data + CHUNK);
-    s.src = reinterpret_cast<unsigned char**>(s.data + CHUNK + em_far_bytes(HD, slabs));
-    s.dst = s.src + rows;
-    s.back = reinterpret_cast<int*>(s.dst + rows);
+    s.far = reinterpret_cast<float*>(s.data + chunk);
+    s.src = reinterpret_cast<unsigned char**>(s.data + chunk + (keys ? em_far_bytes(HD, slabs) : 0));
+    s.dst = s.src + 32;
+    s.back = reinterpret_cast<int*>(s.dst + 32);
     return s;
   };
   if (rope && tid < F) speeds[tid] = sh.speeds[slab * F + tid];
   if (tid == 0) {
     for (int i = 0; i < stages; ++i) {
       mbar_init(&full[i], 64);  // every lane of the reader, once for what it wrote and once for its copies
-      mbar_init(&empty[i], EM_WRITERS);
+      mbar_init(&empty[i], 1);
     }
+    arrived = 0;
     fence_mbar_init();
   }
   pdl_trigger();
@@ -252,150 +259,173 @@ __global__ void __launch_bounds__(EM_THREADS) evict_move_kernel(const EvictArgs 
     entry[F + at] = a.y;
   };
   if (rope)
-    for (int i = tid; i < 64 * F; i += EM_THREADS) enter(near + i / F * 2 * F, i % F, i / F);
+    for (int i = tid; i < 64 * F; i += THREADS) enter(near + i / F * 2 * F, i % F, i / F);
   __syncthreads();
   pdl_wait();
-  const int chunks = (e.k + rows - 1) / rows;
+  const int chunks = (e.k + 31) / 32;
   const int pieces = bytes / 16, half = keys ? pieces / 2 : pieces;  // of a row's slab; those of its first half
   const int shift = 31 - __clz(pieces);
   bool alive = true;
   auto wait = [&](uint64_t* bar, uint32_t parity) { alive = alive && __all_sync(0xffffffffu, mbar_wait(bar, parity, p.status)); };
 
-  if (warp >= EM_WRITERS) {  // ---- requests ----
+  auto wait_arrived = [&](int n) {
+    const volatile int* a = &arrived;
+#pragma unroll 1
+    for (uint32_t i = 0; alive && *a < n; ++i)
+      if (i == EM_POLLS) {
+        alive = false;
+        atomicOr(p.status + ST_ERR, ERR_TIMEOUT);
+      }
+    __threadfence_block();
+    alive = __all_sync(0xffffffffu, alive);
+  };
+
+  if (warp == ORDER) {  // ---- a lane per chunk of the next ones asks whether it has arrived ----
+    int st = lane, phase = 0, n = 0;  // of the lane's chunk, n + lane; the phase before this one is over: chunk n + lane - stages was seen
+#pragma unroll 1
+    for (uint32_t i = 0; n < chunks && i < EM_POLLS; ++i) {
+      const bool got = lane < stages && n + lane < chunks && mbar_test_wait_at(smem_u32(&full[st]), phase);
+      const int more = __ffs((int)~__ballot_sync(0xffffffffu, got)) - 1;  // at most the stages: fewer than 32
+      if (more == 0) continue;
+      i = 0;
+      n += more;
+      st += more;
+      if (st >= stages) {
+        st -= stages;
+        phase ^= 1;
+      }
+      __threadfence_block();
+      if (lane == 0) *const_cast<volatile int*>(&arrived) = n;
+    }
+    if (n < chunks && lane == 0) atomicOr(p.status + ST_ERR, ERR_TIMEOUT);
+    return;
+  }
+
+  if (warp >= WRITERS) {  // ---- requests ----
     const int32_t *table = p.kv.page_table + (size_t)b * mp, *dst_table = p.dst_table + (size_t)b * mp;
     unsigned char* pool = static_cast<unsigned char*>(keys ? p.kv.k_pool : p.kv.v_pool);
     const int first = slab * half * 16;
-    int next[4];  // kept tokens of this lane's rows
+    int next;  // kept token of this lane's row
     auto look = [&](int c) {
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int j = c * rows + x * 32 + lane;
-        next[x] = x < slabs && j < e.k ? kept[j] : -1;
-      }
+      const int j = c * 32 + lane;
+      next = j < e.k ? kept[j] : -1;
     };
-    // No more readers than stages: a reader that waits for chunk c - stages to leave has seen chunk c - readers - stages leave, so
-    // the phase before the one it waits for is over (the parity of a phase does not tell it from the one after the next).
-    const int readers = min(EM_READERS, stages);
-    int c = warp - EM_WRITERS;
-    if (c >= readers) return;
+    int c = warp - WRITERS, st = c, phase = 1;  // phase: of the stage's `empty`; the first use waits for none
     look(c);
 #pragma unroll 1
-    for (; c < chunks; c += readers) {
-      const int st = c % stages;
+    for (; c < chunks; c += READERS) {
       const Stage s = stage(st);
-      unsigned char *src[4], *dst[4];
-      int low = 0x7fffffff, top = 0, back[4];
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int i = next[x], j = c * rows + x * 32 + lane;
-        src[x] = dst[x] = nullptr;
-        back[x] = 0;
-        if (i < 0) continue;
+      unsigned char *src = nullptr, *dst = nullptr;
+      const int i = next, j = c * 32 + lane, back = i < 0 ? 0 : i - j;
+      if (i >= 0) {
         const int from = table[i / PAGE], to = dst_table[j / PAGE];
-        back[x] = i - j;
-        low = min(low, back[x] >> 6);
-        top = max(top, back[x] >> 6);
         if ((unsigned)from >= (unsigned)p.kv.num_pages || (unsigned)to >= (unsigned)p.kv.num_pages) {
           atomicOr(p.status + ST_ERR, ERR_BAD_PAGE);
-          continue;
+        } else {
+          src = pool + (((size_t)from * Hkv + kvh) * PAGE + i % PAGE) * ROW + first;
+          dst = pool + (((size_t)to * Hkv + kvh) * PAGE + j % PAGE) * ROW + first;
+          if (src == dst) src = dst = nullptr;  // it stays where it is
         }
-        src[x] = pool + (((size_t)from * Hkv + kvh) * PAGE + i % PAGE) * ROW + first;
-        dst[x] = pool + (((size_t)to * Hkv + kvh) * PAGE + j % PAGE) * ROW + first;
-        if (src[x] == dst[x]) src[x] = dst[x] = nullptr;  // it stays where it is
       }
-      look(c + readers);
-      if (c >= stages) wait(&empty[st], (c / stages - 1) & 1);
+      look(c + READERS);
+      if (c >= stages) {
+        wait_arrived(c - stages + 1);  // so the stage has been left once less than is asked for next, and no phase is mistaken
+        wait(&empty[st], phase);
+      }
       if (!alive) break;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        if (x >= slabs) break;
-        s.src[x * 32 + lane] = src[x];
-        s.dst[x * 32 + lane] = dst[x];
-        s.back[x * 32 + lane] = back[x];
-      }
+      s.src[lane] = src;
+      s.dst[lane] = dst;
+      s.back[lane] = back;
       __syncwarp();
       const uint32_t data = smem_u32(s.data);
 #pragma unroll 8
-      for (int t = lane; t < CHUNK / 16; t += 32) {
+      for (int t = lane; t < 2 * bytes; t += 32) {
         const int r = t >> shift, q = t - (r << shift);
         const unsigned char* from = s.src[r];
         if (from) em_copy16(data + t * 16, from + (q < half ? q * 16 : ROW / 2 + (q - half) * 16));
       }
       if (rope) {
-        low = __reduce_min_sync(0xffffffffu, low);
-        top = __reduce_max_sync(0xffffffffu, top);
+        const int low = __reduce_min_sync(0xffffffffu, i < 0 ? 0x7fffffff : back >> 6), top = __reduce_max_sync(0xffffffffu, back >> 6);
         const bool fits = top - low < EM_FAR;
         if (fits)
-          for (int m = low; m <= top; ++m)
-            for (int f = lane; f < F; f += 32) enter(s.far + (m - low) * 2 * F, f, m * 64);
+          for (int x = lane; x < (top - low + 1) * F; x += 32) enter(s.far + x / F * 2 * F, x % F, (low + x / F) * 64);
         if (lane == 0) far0[st] = fits ? low : -1;
       }
       asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&full[st])) : "memory");
       mbar_arrive(&full[st]);
+      st += READERS;
+      if (st >= stages) {
+        st -= stages;
+        phase ^= 1;
+      }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");  // also where a wait gave up: nothing is in flight when the CTA ends
     return;
   }
 
-  // ---- a warp writes every eighth chunk, and sees the others arrive ----
+  // ---- a warp writes a chunk when it and all before it have arrived ----
+  int st = warp, phase = 0;
 #pragma unroll 1
-  for (int c = 0; c < chunks; ++c) {
-    const int st = c % stages;
-    wait(&full[st], (c / stages) & 1);
+  for (int c = warp; c < chunks; c += WRITERS) {
+    wait_arrived(c + 1);
+    wait(&full[st], phase);  // (it has; now this warp has seen it)
     if (!alive) break;
-    if (c % EM_WRITERS == warp) {
-      const Stage s = stage(st);
-      const uint4* data = reinterpret_cast<const uint4*>(s.data);
-      if (!rope) {
+    const Stage s = stage(st);
+    const uint4* data = reinterpret_cast<const uint4*>(s.data);
+    if (!rope) {
 #pragma unroll 4
-        for (int t = lane; t < CHUNK / 16; t += 32) {
-          const int r = t >> shift, q = t - (r << shift);
-          unsigned char* to = s.dst[r];
-          if (to) *reinterpret_cast<uint4*>(to + (q < half ? q * 16 : ROW / 2 + (q - half) * 16)) = data[t];
-        }
-      } else {
-        const int f0 = lane % half, low = far0[st];
+      for (int t = lane; t < 2 * bytes; t += 32) {
+        const int r = t >> shift, q = t - (r << shift);
+        unsigned char* to = s.dst[r];
+        if (to) *reinterpret_cast<uint4*>(to + (q < half ? q * 16 : ROW / 2 + (q - half) * 16)) = data[t];
+      }
+    } else {
+      const int f0 = lane % half, low = far0[st];
 #pragma unroll 2
-        for (int r = lane / half; r < rows; r += 32 / half) {
-          uint4* dst = reinterpret_cast<uint4*>(s.dst[r]);
-          if (dst == nullptr) continue;
-          const int back = s.back[r];
-          const uint4 lo = data[r * pieces + f0], hi = data[r * pieces + half + f0];
-          const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, h[4] = {hi.x, hi.y, hi.z, hi.w};
-          uint32_t new_l[4], new_h[4];
-          const float *a = near + (back & 63) * 2 * F + f0 * 4, *w = s.far + ((back >> 6) - max(low, 0)) * 2 * F + f0 * 4;
+      for (int r = lane / half; r < 32; r += 32 / half) {
+        uint4* dst = reinterpret_cast<uint4*>(s.dst[r]);
+        if (dst == nullptr) continue;
+        const int back = s.back[r];
+        const uint4 lo = data[r * pieces + f0], hi = data[r * pieces + half + f0];
+        const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, h[4] = {hi.x, hi.y, hi.z, hi.w};
+        uint32_t new_l[4], new_h[4];
+        const float *a = near + (back & 63) * 2 * F + f0 * 4, *w = s.far + ((back >> 6) - max(low, 0)) * 2 * F + f0 * 4;
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {  // four pairs at a time
-            float cs[4], sn[4];
-            if (low >= 0) {
-              const float4 ac = *reinterpret_cast<const float4*>(a + q * F / 2), as = *reinterpret_cast<const float4*>(a + F + q * F / 2);
-              const float4 wc = *reinterpret_cast<const float4*>(w + q * F / 2), ws = *reinterpret_cast<const float4*>(w + F + q * F / 2);
-              cs[0] = wc.x * ac.x - ws.x * as.x; sn[0] = ws.x * ac.x + wc.x * as.x;
-              cs[1] = wc.y * ac.y - ws.y * as.y; sn[1] = ws.y * ac.y + wc.y * as.y;
-              cs[2] = wc.z * ac.z - ws.z * as.z; sn[2] = ws.z * ac.z + wc.z * as.z;
-              cs[3] = wc.w * ac.w - ws.w * as.w; sn[3] = ws.w * ac.w + wc.w * as.w;
-            } else {
+        for (int q = 0; q < 2; ++q) {  // four pairs at a time
+          float cs[4], sn[4];
+          if (low >= 0) {
+            const float4 ac = *reinterpret_cast<const float4*>(a + q * F / 2), as = *reinterpret_cast<const float4*>(a + F + q * F / 2);
+            const float4 wc = *reinterpret_cast<const float4*>(w + q * F / 2), ws = *reinterpret_cast<const float4*>(w + F + q * F / 2);
+            cs[0] = wc.x * ac.x - ws.x * as.x; sn[0] = ws.x * ac.x + wc.x * as.x;
+            cs[1] = wc.y * ac.y - ws.y * as.y; sn[1] = ws.y * ac.y + wc.y * as.y;
+            cs[2] = wc.z * ac.z - ws.z * as.z; sn[2] = ws.z * ac.z + wc.z * as.z;
+            cs[3] = wc.w * ac.w - ws.w * as.w; sn[3] = ws.w * ac.w + wc.w * as.w;
+          } else {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const float2 t = turn_back((uint32_t)back, speeds[f0 * 8 + q * 4 + i]);
-                cs[i] = t.x;
-                sn[i] = t.y;
-              }
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const float l0 = bf16_lo(l[2 * q + i]), l1 = bf16_hi(l[2 * q + i]), h0 = bf16_lo(h[2 * q + i]), h1 = bf16_hi(h[2 * q + i]);
-              new_l[2 * q + i] = em_pack(l0 * cs[2 * i] - h0 * sn[2 * i], l1 * cs[2 * i + 1] - h1 * sn[2 * i + 1]);
-              new_h[2 * q + i] = em_pack(h0 * cs[2 * i] + l0 * sn[2 * i], h1 * cs[2 * i + 1] + l1 * sn[2 * i + 1]);
+            for (int i = 0; i < 4; ++i) {
+              const float2 t = turn_back((uint32_t)back, speeds[f0 * 8 + q * 4 + i]);
+              cs[i] = t.x;
+              sn[i] = t.y;
             }
           }
-          dst[f0] = back ? make_uint4(new_l[0], new_l[1], new_l[2], new_l[3]) : lo;
-          dst[f0 + ROW / 32] = back ? make_uint4(new_h[0], new_h[1], new_h[2], new_h[3]) : hi;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float l0 = bf16_lo(l[2 * q + i]), l1 = bf16_hi(l[2 * q + i]), h0 = bf16_lo(h[2 * q + i]), h1 = bf16_hi(h[2 * q + i]);
+            new_l[2 * q + i] = em_pack(l0 * cs[2 * i] - h0 * sn[2 * i], l1 * cs[2 * i + 1] - h1 * sn[2 * i + 1]);
+            new_h[2 * q + i] = em_pack(h0 * cs[2 * i] + l0 * sn[2 * i], h1 * cs[2 * i + 1] + l1 * sn[2 * i + 1]);
+          }
         }
+        dst[f0] = back ? make_uint4(new_l[0], new_l[1], new_l[2], new_l[3]) : lo;
+        dst[f0 + ROW / 32] = back ? make_uint4(new_h[0], new_h[1], new_h[2], new_h[3]) : hi;
       }
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(&empty[st]);
+    st += WRITERS;
+    if (st >= stages) {
+      st -= stages;
+      phase ^= 1;
+    }
   }
 }
 
@@ -403,7 +433,9 @@ template <int HD>
 static void launch_move(const EvictArgs& a, cudaStream_t st) {
   const int Hkv = a.shape.n_kv_heads, rows = 2 * a.B * Hkv;
   MoveShape sh;
-  sh.slabs = rows >= sm_count() ? HD / 64 : HD / 32;  // pieces of 64 bytes of a key; of 32 where CTAs are few
+  // Pieces of 64 bytes of a key, or of 32 where every CTA then still has an SM to itself (four sequences of 8000: 41 us with pieces
+  // of 64 and an SM each, 56 with pieces of 32 and two CTAs an SM)
+  sh.slabs = rows * (HD / 32) > sm_count() ? HD / 64 : HD / 32;
   for (int f = 0; f < 64; ++f) sh.speeds[f] = make_uint2(0, 0);
   if (a.shape.rope_theta > 0.f)
     for (int f = 0; f < HD / 2; ++f) {
@@ -411,12 +443,14 @@ static void launch_move(const EvictArgs& a, cudaStream_t st) {
       const uint64_t fraction = (uint64_t)((turns - floor(turns)) * 0x1p64);
       sh.speeds[f] = make_uint2((uint32_t)fraction, (uint32_t)(fraction >> 32));
     }
-  const int each = em_stage_bytes(HD, sh.slabs), tables = 64 * 2 * (HD / 2 / sh.slabs) * 4;
-  const int room = (rows * sh.slabs > sm_count() ? 100 : 200) * 1024;  // two CTAs per SM where there are so many
-  sh.stages = std::min(EM_MAX_STAGES, (room - tables) / each);
-  const int smem = sh.stages * each + tables;
-  ensure_dynamic_smem(reinterpret_cast<const void*>(&evict_move_kernel<HD>), smem);
-  SOL_LAUNCH("evict_move", evict_move_kernel<HD>, dim3(2 * sh.slabs, Hkv, a.B), dim3(EM_THREADS), smem, st, a, sh);
+  const bool two = rows * sh.slabs > sm_count();  // CTAs per SM
+  const int near = em_near_bytes(HD, sh.slabs), room = (two ? 108 : 216) * 1024;
+  sh.key_stages = std::min(EM_MAX_STAGES, (room - near) / em_stage_bytes(HD, sh.slabs, true));  // at least as many as readers, writers
+  sh.value_stages = std::min(EM_MAX_STAGES, room / em_stage_bytes(HD, sh.slabs, false));
+  const int smem = std::max(near + sh.key_stages * em_stage_bytes(HD, sh.slabs, true), sh.value_stages * em_stage_bytes(HD, sh.slabs, false));
+  const auto kernel = two ? evict_move_kernel<HD, EM_FEW> : evict_move_kernel<HD, EM_MANY>;
+  ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
+  SOL_LAUNCH("evict_move", kernel, dim3(2 * sh.slabs, Hkv, a.B), dim3((2 * (two ? EM_FEW : EM_MANY) + 2) * 32), smem, st, a, sh);
 }
 
 void launch_evict(const EvictArgs& a, cudaStream_t st) {
