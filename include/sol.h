@@ -335,6 +335,7 @@ size_t sol_tree_workspace_bytes(const sol_shape_t *shape, int32_t max_batch, int
  * the page selection do not act here.  What a masked node's key and value hold, numbers or not, does not reach a row that
  * does not see it; neither do slots behind the sequence.  Tokens of a page whose number is out of range are skipped and
  * raise the status bit.  At most 256 kv-heads.
+ * Scores, maxima and sums are float32; the weights are rounded to bf16 for the product with V.
  *   q_bf16 [B][max_nodes][n_q][head_dim] (already rotated); out_bf16 the same shape. */
 sol_status_t sol_tree_attn(const sol_shape_t *shape, const void *q_bf16, const sol_kv_t *kv, const sol_tree_t *tree, int32_t B,
                            void *out_bf16, void *ws, size_t ws_bytes, sol_stream_t stream);
@@ -350,8 +351,8 @@ sol_status_t sol_tree_accept(int32_t B, int32_t max_nodes, const int32_t *n_node
  * nodes' slots are then free.  (A node of depth j was rotated for that position.)  The path must ascend; it ends at the
  * first entry that does not, or that is no node, which raises the bad-action bit.
  *   kvs: HOST array of n_layers structs; tree: n_nodes and max_nodes (the mask may be NULL); new_lens [B] out, optional:
- *   the lengths of kvs[0] afterwards; it must not overlap any seq_lens; ws: an initialised workspace of any size (its
- *   status words). */
+ *   the lengths of kvs[0] afterwards; it must not overlap any seq_lens, n_nodes or path_len; ws: an initialised workspace of
+ *   any size (its status words).  The pages that hold the drafted nodes must belong to their sequence alone. */
 sol_status_t sol_tree_commit(const sol_shape_t *shape, int32_t n_layers, const sol_kv_t *kvs, const sol_tree_t *tree, int32_t B,
                              const int32_t *path, const int32_t *path_len, int32_t *new_lens, void *ws, sol_stream_t stream);
 
@@ -371,10 +372,12 @@ sol_status_t sol_weighted_decode_attn(const sol_shape_t *shape, const void *q_bf
  * rotated by j - i positions (in float32, rounded to bf16), so that every slot t holds a key at position t, as
  * sol_decode_layer expects of the cache it appends to; without it keys are copied.
  *   budgets [B]; weights, dst_weights float32 [B][n_kv][max_pages_per_seq * page_size]; dst_table int32
- *   [B][max_pages_per_seq], of the same pools; dst_lens [B] out: the new lengths; it must not overlap kv->seq_lens;
+ *   [B][max_pages_per_seq], of the same pools; dst_lens [B] out: the new lengths; it must not overlap kv->seq_lens or budgets;
  *   kept_idx (optional) int32 [B][n_kv][max_pages_per_seq * page_size] out: the kept tokens' old slots, ascending.
- * In place: dst_table may be kv->page_table (or hold the same pages in the same places) and dst_weights may be weights.
- * Otherwise the destinations must not overlap what any sequence of the batch still reads.  The Quest extrema are not updated:
+ * In place: dst_table may be kv->page_table (or hold the same pages in the same places) and dst_weights may be weights;
+ * the pages then must belong to their sequence alone.  Otherwise the destinations must not overlap each other or what any
+ * sequence of the batch still reads.  A row whose old or new page is out of range is left where it is and raises the status
+ * bit.  The Quest extrema are not updated:
  * call sol_quest_build_meta afterwards.  ws: sol_workspace_bytes.  At most 256 kv-heads. */
 sol_status_t sol_kv_evict(const sol_shape_t *shape, const sol_kv_t *kv, int32_t B, const int32_t *budgets, const float *weights,
                           const int32_t *dst_table, float *dst_weights, int32_t *dst_lens, int32_t *kept_idx, void *ws,

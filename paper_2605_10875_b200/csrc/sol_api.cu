@@ -793,6 +793,12 @@ static bool cache_size_ok(const sol_shape_t* s, const sol_kv_t* kv) {
          (long long)kv->num_pages * s->n_kv_heads * PAGE < (1ll << 31);
 }
 static bool tree_ok(const sol_tree_t* t) { return t && t->n_nodes && t->mask && t->max_nodes >= 1; }
+static bool aligned8(const void* a) { return (reinterpret_cast<uintptr_t>(a) & 7) == 0; }
+// Do B int32 at a share any with those at b?  (An output that other CTAs of the call still read as an input.)
+static bool share_ints(const void* a, const void* b, int B) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + (size_t)B * 4 && y < x + (size_t)B * 4;
+}
 
 // Which kernel takes a tree: a block of 16 query rows goes through mma.sync, more rows through tcgen05.
 static bool tree_by_rows(const sol_shape_t* s, int max_nodes) { return max_nodes * (s->n_q_heads / s->n_kv_heads) <= 16; }
@@ -806,7 +812,7 @@ size_t sol_tree_workspace_bytes(const sol_shape_t* shape, int32_t max_batch, int
 
 sol_status_t sol_tree_build(int32_t B, int32_t max_nodes, const int32_t* n_nodes, const int32_t* parents, uint64_t* mask,
                             int32_t* depth, sol_stream_t stream) {
-  if (!n_nodes || !parents || !mask || B < 0 || max_nodes < 1) return SOL_ERR_INVALID_ARG;
+  if (!n_nodes || !parents || !mask || !aligned8(mask) || B < 0 || max_nodes < 1) return SOL_ERR_INVALID_ARG;
   if (max_nodes > MAX_TREE_NODES) return SOL_ERR_UNSUPPORTED;
   if (B == 0) return SOL_OK;
   launch_tree_build(B, max_nodes, n_nodes, parents, mask, depth, (cudaStream_t)stream);
@@ -816,7 +822,8 @@ sol_status_t sol_tree_build(int32_t B, int32_t max_nodes, const int32_t* n_nodes
 sol_status_t sol_tree_attn(const sol_shape_t* shape, const void* q_bf16, const sol_kv_t* kv, const sol_tree_t* tree, int32_t B,
                            void* out_bf16, void* ws, size_t ws_bytes, sol_stream_t stream) {
   if (!shape || !q_bf16 || !kv_ok(kv) || !tree_ok(tree) || !out_bf16 || !ws || B < 0) return SOL_ERR_INVALID_ARG;
-  if (!aligned16(q_bf16) || !aligned16(out_bf16) || !aligned16(kv->k_pool) || !aligned16(kv->v_pool) || !aligned16(ws))
+  if (!aligned16(q_bf16) || !aligned16(out_bf16) || !aligned16(kv->k_pool) || !aligned16(kv->v_pool) || !aligned16(ws) ||
+      !aligned8(tree->mask))
     return SOL_ERR_INVALID_ARG;
   if (!shape_ok(shape) || B > 128 || !cache_size_ok(shape, kv) || tree->max_nodes > MAX_TREE_NODES) return SOL_ERR_UNSUPPORTED;
   if (B == 0) return SOL_OK;
@@ -848,8 +855,10 @@ sol_status_t sol_tree_commit(const sol_shape_t* shape, int32_t n_layers, const s
                              const int32_t* path, const int32_t* path_len, int32_t* new_lens, void* ws, sol_stream_t stream) {
   if (!shape || n_layers < 1 || !kvs || !tree || !tree->n_nodes || tree->max_nodes < 1 || !path || !path_len || !ws || B < 0)
     return SOL_ERR_INVALID_ARG;
+  if (!aligned16(ws) || share_ints(new_lens, tree->n_nodes, B) || share_ints(new_lens, path_len, B)) return SOL_ERR_INVALID_ARG;
   for (int l = 0; l < n_layers; ++l)
-    if (!kv_ok(&kvs[l]) || !aligned16(kvs[l].k_pool) || !aligned16(kvs[l].v_pool)) return SOL_ERR_INVALID_ARG;
+    if (!kv_ok(&kvs[l]) || !aligned16(kvs[l].k_pool) || !aligned16(kvs[l].v_pool) || share_ints(new_lens, kvs[l].seq_lens, B))
+      return SOL_ERR_INVALID_ARG;
   if (!shape_ok(shape) || B > 128 || tree->max_nodes > MAX_TREE_NODES) return SOL_ERR_UNSUPPORTED;
   for (int l = 0; l < n_layers; ++l)
     if (!cache_size_ok(shape, &kvs[l])) return SOL_ERR_UNSUPPORTED;
@@ -886,7 +895,9 @@ sol_status_t sol_kv_evict(const sol_shape_t* shape, const sol_kv_t* kv, int32_t 
                           size_t ws_bytes, sol_stream_t stream) {
   if (!shape || !kv_ok(kv) || !budgets || !weights || !dst_table || !dst_weights || !dst_lens || !ws || B < 0)
     return SOL_ERR_INVALID_ARG;
-  if (!aligned16(kv->k_pool) || !aligned16(kv->v_pool) || !aligned16(ws) || dst_lens == kv->seq_lens) return SOL_ERR_INVALID_ARG;
+  if (!aligned16(kv->k_pool) || !aligned16(kv->v_pool) || !aligned16(ws) || share_ints(dst_lens, kv->seq_lens, B) ||
+      share_ints(dst_lens, budgets, B))
+    return SOL_ERR_INVALID_ARG;
   if (!shape_ok(shape) || B > 128 || !cache_size_ok(shape, kv)) return SOL_ERR_UNSUPPORTED;
   if (B == 0) return SOL_OK;
   const Layout L = make_layout(*shape, B, kv->max_pages_per_seq);

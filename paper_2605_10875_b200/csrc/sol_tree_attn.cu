@@ -259,9 +259,8 @@ __device__ void tree_clear(const TreeDev& p, TreeShared<HD>& sh, uint32_t v_ring
 
 // ---- tensor cores ----
 // This warp's pace is the kernel's.  It waits without naps (mbar_test_wait_at) for all that a step needs at once, a barrier per
-// lane, and issues a step's products
-// and commits in one elected block on operands that are the same in all lanes: 32 to 62 cycles a product, where predicated ones
-// took 80 and blocks on lanes' own values more than that.
+// lane, and issues a step's products and commits in one elected block on operands that are the same in all lanes: 32 to 62 cycles
+// a product, where predicated ones took 80 and blocks on lanes' own values more than that.
 template <int HD>
 __device__ void tree_mma(const TreeDev& p, TreeShared<HD>& sh, uint32_t q_oper, uint32_t k_ring, uint32_t v_ring, int u0, int u1) {
   using Z = TaSize<HD>;
@@ -270,7 +269,8 @@ __device__ void tree_mma(const TreeDev& p, TreeShared<HD>& sh, uint32_t q_oper, 
   const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
   const uint64_t q_desc = umma_smem_desc(q_oper, 16, 1024);
   const uint64_t k_desc = umma_smem_desc(k_ring, 16, 1024), v_desc = umma_smem_desc(v_ring, Z::CHUNK, 1024);
-  const uint32_t k_full = smem_u32(sh.k_full), v_full = smem_u32(sh.v_full), v_clean = smem_u32(sh.v_clean), p_half = smem_u32(sh.p_half), p_ready = smem_u32(sh.p_ready);
+  const uint32_t k_full = smem_u32(sh.k_full), v_full = smem_u32(sh.v_full), v_clean = smem_u32(sh.v_clean);
+  const uint32_t p_half = smem_u32(sh.p_half), p_ready = smem_u32(sh.p_ready);
   bool alive = true;
   auto wait = [&](uint32_t bar, uint32_t parity) {  // bar, parity: this lane's.  After one that gave up, the others return at once
     if (!alive) return;

@@ -107,6 +107,23 @@ def test_kv_evict_refuses():
                (sol.SOL_OK, call(B=0))] + [(U, call(shape=_shape(**s))) for s in BAD_SHAPES])
 
 
+def test_outputs_that_share_an_input_and_misaligned_words_are_refused():
+    I = sol.SOL_ERR_INVALID_ARG
+
+    def commit(lens, n=0x3000, count=0x4000, kvs=None, ws=FAKE):
+        return lambda: sol.tree_commit(_shape(), kvs or [_kv(seq_lens=0x2000)], sol.make_tree(8, n), 4, FAKE, count, lens, ws,
+                                       check=False)
+
+    def evict(lens):
+        return lambda: sol.kv_evict(_shape(), _kv(seq_lens=0x2000), 4, 0x3000, FAKE, FAKE, FAKE, lens, None, FAKE, BIG, check=False)
+
+    _refusals([(I, commit(0x2000)), (I, commit(0x200C)), (I, commit(0x1FF4)), (I, commit(0x3000)), (I, commit(0x400C)),
+               (I, commit(0x5000, kvs=[_kv(seq_lens=0x2000), _kv(seq_lens=0x5004)])), (I, commit(0x5000, ws=FAKE + 4)),
+               (I, evict(0x2004)), (I, evict(0x1FF4)), (I, evict(0x3008)),
+               (I, lambda: sol.tree_build(2, 4, FAKE, FAKE, FAKE + 4, None, check=False)),
+               (I, lambda: sol.tree_attn(_shape(), FAKE, _kv(), sol.make_tree(8, FAKE, FAKE + 4), 2, FAKE, FAKE, BIG, check=False))])
+
+
 # ---- pins of the oracle --------------------------------------------------------------------------
 def _cache(lens, seed=0, theta=0.0):
     cfg = dict(synth.WORKLOADS["tiny"], shuffle_pages=True)

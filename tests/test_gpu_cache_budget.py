@@ -14,6 +14,8 @@ from tests import harness as H
 
 pytestmark = pytest.mark.gpu
 
+MAX_PAGES = 768  # of a sequence
+
 
 class Weighted:
     def __init__(self, heads, lens, seed=0, decay=1.0, pages=None):
@@ -242,6 +244,69 @@ def test_evict_reports_bad_pages():
     c.dst_table[0, 1] = c.kv.num_pages
     c.launch()
     assert c.ws.status()[0] == 2 and int(c.dst_lens[0]) == 100
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("heads,B", [("g1", 19), ("g3", 128), ("g4", 19), ("g8", 40), ("g4", 18)])
+def test_evict_many_rows(heads, B, in_place):
+    """Batches on both sides of where two CTAs share an SM, up to the largest."""
+    lens = [(37 * b * b + 5 * b) % 300 for b in range(B)]
+    Evict(heads, lens, [(b * 53) % 250 for b in range(B)], in_place=in_place, seed=10).check((heads, B, in_place))
+
+
+@pytest.mark.parametrize("heads", ["g2", "g4"])
+def test_evict_the_longest_row(heads):
+    """A full page table of the largest size, next to an empty sequence and one of a single token."""
+    T = MAX_PAGES * 64
+    Evict(heads, [T, 0, 1], [20000, 5, 1], theta=500000.0, in_place=True, seed=11, sink=4, window=100).check("long")
+
+
+def test_weighted_the_longest_row_and_the_largest_batch():
+    Weighted("g2", [MAX_PAGES * 64], decay=0.5).check("long")
+    Weighted("g6", [(31 * b) % 200 for b in range(128)], seed=3, decay=0.5).check("wide")
+
+
+def test_two_streams_at_once_with_workspaces_of_their_own():
+    """Runs on two streams at the same time give what each gives alone."""
+    def run(c, e, stream):
+        c.launch(stream)
+        e.launch(stream)
+
+    alone = [(Weighted("g4", [900, 40, 3000], seed=s, decay=0.5), Evict("g4", [2500, 700], [1000, 300], seed=s)) for s in (20, 21)]
+    both = [(Weighted("g4", [900, 40, 3000], seed=s, decay=0.5), Evict("g4", [2500, 700], [1000, 300], seed=s)) for s in (20, 21)]
+    for c, e in alone:
+        run(c, e, None)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in both]
+    for (c, e), s in zip(both, streams):
+        run(c, e, s)
+    torch.cuda.synchronize()
+    for (c, e), (c2, e2) in zip(alone, both):
+        assert torch.equal(c.out.view(torch.int16), c2.out.view(torch.int16))
+        assert torch.equal(c.weights.view(torch.int32), c2.weights.view(torch.int32))  # bits: NaN equals NaN
+        assert torch.equal(e.kept, e2.kept) and torch.equal(e.dst_lens, e2.dst_lens)
+        assert torch.equal(e.kv.k_pool.view(torch.int16), e2.kv.k_pool.view(torch.int16))
+        assert c2.ws.status()[0] == 0 and e2.ws.status()[0] == 0
+
+
+def test_evict_captured_and_replayed_with_other_budgets():
+    c = Evict("g8", [800, 130], [300, 100], seed=12)
+    pools = c.kv.k_pool.clone(), c.kv.v_pool.clone()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        c.launch(torch.cuda.current_stream())
+    for budgets, w_seed in (([300, 100], 0), ([799, 5], 1), ([10, 500], 2)):
+        c.kv.k_pool.copy_(pools[0])
+        c.kv.v_pool.copy_(pools[1])
+        c.budgets = budgets
+        c.dev_budgets.copy_(H.dev_i32(budgets))
+        c.old_w = np.random.default_rng(w_seed).exponential(1.0, c.old_w.shape).astype(np.float32)
+        c.weights.copy_(torch.from_numpy(c.old_w))
+        c.kept.fill_(-1)
+        c.launch = lambda: (g.replay(), torch.cuda.synchronize())
+        c.check(budgets)
 
 
 def test_a_serving_loop_with_a_tree_and_a_budget():

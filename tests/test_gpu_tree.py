@@ -221,6 +221,27 @@ def test_captured_and_replayed_with_other_lengths():
             assert np.all(got[b, n:] == FILL)
 
 
+def test_the_longest_context_and_the_largest_batch():
+    Case("g2", [768 * 64 - 64], [64], 64, seed=15).check("long")
+    Case("g4", [768 * 64 - 3], [3], 3, seed=16).check("long, few rows")
+    Case("g6", [(29 * b) % 150 for b in range(128)], [(7 * b) % 65 if b % 5 else 0 for b in range(128)], 64, seed=17).check("wide")
+
+
+def test_two_streams_at_once_with_workspaces_of_their_own():
+    make = lambda: [Case("g8", [900, 40], [33, 64], 64, seed=18), Case("g2", [2000, 7, 300], [5, 8, 1], 8, seed=19)]  # noqa: E731
+    alone, both = make(), make()
+    for c in alone:
+        c.launch()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in both]
+    for _ in range(3):
+        for c, s in zip(both, streams):
+            c.launch(stream=s)
+    torch.cuda.synchronize()
+    for a, b in zip(alone, both):
+        assert np.array_equal(H.host_u16(a.out), H.host_u16(b.out)) and b.ws.status()[0] == 0
+
+
 # ---- bookkeeping ---------------------------------------------------------------------------------
 @pytest.mark.parametrize("N,near", [(1, 1), (2, 1), (33, 5), (64, 1), (64, 8), (64, 64)])
 def test_build_matches_the_walk_up(N, near):
@@ -312,3 +333,46 @@ def test_commit_reports_paths_that_do_not_ascend_and_bad_pages():
     sol.workspace_init(ws, 256)
     sol.tree_commit(shape, [kv.struct()], tree, 4, H.dev_i32(path), H.dev_i32([2, 1, 1, 1]), None, ws)
     assert sol.read_device_status(ws)[0] & 2
+
+
+def test_a_whole_step_captured_and_replayed():
+    """Masks, attention, acceptance and commit as one graph, replayed on other trees, against the calls one by one."""
+    B, N = 3, 20
+    rng = np.random.default_rng(5)
+    c = Case("g4", [90, 200, 64], [20, 7, 13], N, seed=20)
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device=H.DEV)  # noqa: E731
+    parents, draft, target, path, count, token, new = i32(B, N), i32(B, N), i32(B, N), i32(B, N), i32(B), i32(B), i32(B)
+
+    def step(stream):
+        tree = sol.make_tree(N, c.n_nodes, c.dmask)
+        sol.tree_build(B, N, c.n_nodes, parents, c.dmask, stream=stream)
+        c.launch(stream=stream)
+        sol.tree_accept(B, N, c.n_nodes, parents, draft, target, path, count, token, stream=stream)
+        sol.tree_commit(c.shape, [c.kv.struct()], tree, B, path, count, new, c.ws.buf, stream)
+
+    pools = c.kv.k_pool.clone(), c.kv.v_pool.clone()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        step(torch.cuda.current_stream())
+    for counts in ([20, 7, 13], [1, 20, 0]):
+        c.n_nodes.copy_(H.dev_i32(counts))
+        parents.copy_(H.dev_i32(CC.random_trees(rng, counts, N, 3)))
+        for x in (draft, target):
+            x.copy_(H.dev_i32(rng.integers(0, 2, (B, N)).astype(np.int32)))
+        results = []
+        for go in (lambda: step(None), g.replay):
+            c.kv.k_pool.copy_(pools[0])
+            c.kv.v_pool.copy_(pools[1])
+            for x in (path, count, token, new):
+                x.fill_(-1)
+            c.out.zero_()
+            torch.cuda.synchronize()
+            go()
+            torch.cuda.synchronize()
+            assert c.ws.status()[0] == 0
+            results.append([x.clone() for x in (path, count, token, new, c.out.view(torch.int16), c.kv.k_pool.view(torch.int16),
+                                                c.kv.v_pool.view(torch.int16))])
+        assert all(torch.equal(a, b) for a, b in zip(*results))
+        assert all(min(1, n) <= int(k) <= n for k, n in zip(results[0][1], counts))
