@@ -5,8 +5,8 @@
 // or two cache pages at a time.  The tiles of all chains, one chain after the other, form one line, of which every CTA takes a
 // run.  A run that ends inside a chain leaves a partial result; a second kernel merges the pieces of chains that were cut.
 // A chain has piece_cost places on the line ahead of its tiles, as many tiles as beginning and ending a piece is worth, so that
-// runs of many short chains are not the longest (128 ragged sequences: 394 us without, 330 with).  Two ways to cut, of which
-// every CTA works out for itself, from the lengths (at most 128), which one is the better:
+// runs of many short chains are not the longest (the attention of 128 ragged decode steps, as it then was: 394 us without, 330
+// with).  Two ways to cut, of which every CTA works out for itself, from the lengths (at most 128), which one is the better:
 //   equal runs       whatever the lengths are.  A run covers the end of one chain, some whole chains and the beginning of another
 //   CTAs per chain   in proportion to its tiles, one at least: every CTA has one piece.  Taken if none is much longer than an equal
 //                    run, where a CTA has the end of one chain and the beginning of another

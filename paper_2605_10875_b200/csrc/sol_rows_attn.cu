@@ -4,12 +4,12 @@
 //   o_r = sum_t p_rt v_t,  p_rt = 2^(s_rt - m_r) / l_r,  s_rt = (q_r . k_t) log2(e) / sqrt(head_dim)  where row r sees token t
 //
 //   rows_attn_kernel   one CTA per SM takes its run of tiles (sol_chain.cuh; a tile is a 64-token page of one kv-head).  A
-//                      producer warp brings keys and values by TMA (128-byte swizzle) in steps of 16 KB, which the other
-//                      warps take in turn, each into its own ring of stages.  Tokens (then head_dim) are the M side of
+//                      producer warp brings a tile's keys and values by TMA (128-byte swizzle) at a time, 16 or 32 KB,
+//                      which the other warps take in turn, each into its own ring of stages.  Tokens (then head_dim) are the M side of
 //                      mma.sync m16n8k16 and the query rows the N side, 16, 8 or 4 of them (S^T = K Q^T, O^T = V^T P^T);
 //                      online softmax in registers, weights as bf16 high and low parts, of four rows in one product.  At
 //                      the end of a chain the warps' results are merged through shared memory.
-//   rows_merge_kernel  merges the chains that were cut between CTAs.
+//   chain_merge_kernel merges the chains that were cut between CTAs.
 //   weight_kernel      the same for decode steps, and then the weights: w_t <- decay w_t + sum_g 2^(s_gt - lse_g) from the
 //                      logits that the first kernel left.
 #include <cuda.h>
@@ -23,7 +23,6 @@
 namespace sol {
 
 constexpr int RA_MAX_ROWS = 16;  // query rows of a chain at most
-constexpr int RA_STAGES = 12;     // of all warps' rings
 constexpr int RA_MIN_TILES = 4;
 constexpr int ra_piece_cost(int hd) { return hd == 64 ? 8 : 4; }
 
@@ -40,22 +39,22 @@ struct RowsDev {
   int* status;
 };
 
-// ROWS query rows per chain: 16, 8 or 4.  Tokens of a step (16 KB of keys and values), bytes of its keys, floats that a lane hands
-// over in a merge.
+// ROWS query rows per chain: 16, 8 or 4.
+// Bound by HBM: one query token of 64 sequences of 8000 of the 8B shape takes 316 us (2.1 GB, 6.6 TB/s; steps of half a tile, in
+// 4 KB boxes, took 403), with 16 rows 32 sequences take 171 us of which the bytes need 161; at head_dim 64 176 of 161.
 template <int HD, int ROWS>
 struct RaSize {
-  static constexpr int TOK = HD == 64 ? 64 : 32;
-  static constexpr int STEPS = PAGE / TOK;     // of a tile
-  static constexpr int HALF = TOK * 128;       // a 64-wide half of the keys: [TOK tokens][128 B]
+  static constexpr int HALF = PAGE * 128;      // a 64-wide half of the keys: [64 tokens][128 B]
   static constexpr int TILE = HALF * (HD / 64);
-  // Consumer warps, stages of a warp's ring: one warp per quarter of the SM (the producer in the fourth) keeps up and has a deep
-  // ring (128 ragged decode steps 340 us, with six warps of two stages 352; 32 chains of 8000 with 16 rows 215 and 222, four warps
-  // 227).  Only 16 rows over the short tiles of head_dim 64 keep three warps busy (16 sequences of 4000: 41 us, with six 37).
-  static constexpr int WARPS = HD == 64 && ROWS == 16 ? 6 : 3, DEPTH = RA_STAGES / WARPS, THREADS = (WARPS + 1) * 32;
+  // Consumer warps, stages of a warp's ring: one warp per quarter of the SM (the producer in the fourth) keeps up and has the
+  // deeper ring (128 ragged decode steps 336 us, with four warps 356, with six 352).  Only 16 rows at head_dim 64 keep three warps busy
+  // (16 sequences of 4000: 41 us, with six 37).
+  static constexpr int STAGES = 192 * 1024 / (2 * TILE), WARPS = HD == 64 && ROWS == 16 ? 6 : 3, DEPTH = STAGES / WARPS;
+  static constexpr int THREADS = (WARPS + 1) * 32;
   static constexpr int NB = ROWS == 16 ? 2 : 1;         // blocks of eight rows
   static constexpr int REGS = (HD / 16 * 4 + 4) * NB;   // sums, two maxima, two sums of weights
   static constexpr int MERGE = 2 * REGS * 32 * 4;
-  static constexpr int SMEM = 1024 + RA_STAGES * 2 * TILE + MERGE;
+  static constexpr int SMEM = 1024 + STAGES * 2 * TILE + MERGE;
 };
 
 // Shared-memory address of 16-byte piece c of token r of a step.
@@ -73,17 +72,18 @@ template <int HD, int ROWS>
 __global__ void __launch_bounds__(RaSize<HD, ROWS>::THREADS, 1)
     rows_attn_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const RowsDev p) {
   using Z = RaSize<HD, ROWS>;
-  constexpr int KS = HD / 16, MT = Z::TOK / 16, NB = Z::NB;  // steps of head_dim, of tokens; blocks of eight rows
+  static_assert(Z::THREADS >= CHAIN_MAX_BATCH, "chain_plan");
+  constexpr int KS = HD / 16, MT = PAGE / 16, NB = Z::NB;  // steps of head_dim, of tokens; blocks of eight rows
   constexpr bool PACK = ROWS == 4;  // rows 4 .. 7 of the block are rows 0 .. 3 again: their weights' low parts
   extern __shared__ unsigned char ra_smem[];
   __shared__ ChainPlan plan;
-  __shared__ uint64_t full[RA_STAGES], empty[RA_STAGES];
-  __shared__ int page_ok[RA_STAGES];
+  __shared__ uint64_t full[Z::STAGES], empty[Z::STAGES];
+  __shared__ int page_ok[Z::STAGES];
   unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(ra_smem) + 1023) & ~(uintptr_t)1023);
-  float* merge = reinterpret_cast<float*>(ring + RA_STAGES * 2 * Z::TILE);
+  float* merge = reinterpret_cast<float*>(ring + Z::STAGES * 2 * Z::TILE);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    for (int s = 0; s < RA_STAGES; ++s) {
+    for (int s = 0; s < Z::STAGES; ++s) {
       mbar_init(&full[s], 1);
       mbar_init(&empty[s], 1);
     }
@@ -107,13 +107,13 @@ __global__ void __launch_bounds__(RaSize<HD, ROWS>::THREADS, 1)
         int mine = 0;
         if (g0 + lane < c.tile1 && c.seq.T > 0) mine = table[g0 + lane];
         const int cnt = min(32, c.tile1 - g0);
-        for (int x = 0; x < cnt * Z::STEPS; ++x, ++it) {
-          int page = __shfl_sync(0xffffffffu, mine, x / Z::STEPS);
+        for (int x = 0; x < cnt; ++x, ++it) {
+          int page = __shfl_sync(0xffffffffu, mine, x);
           // step `it` goes to warp it % Z::WARPS, whose use number `use` of its ring it is
           const int use = it / Z::WARPS, st = it % Z::WARPS * Z::DEPTH + use % Z::DEPTH;
           if (use >= Z::DEPTH && !__all_sync(0xffffffffu, mbar_wait(&empty[st], (use / Z::DEPTH - 1) & 1, p.status))) {
             // the consumers give up too; what has been requested still arrives before the CTA ends
-            for (int i = max(0, it - RA_STAGES); i < it; ++i)
+            for (int i = max(0, it - Z::STAGES); i < it; ++i)
               mbar_wait(&full[i % Z::WARPS * Z::DEPTH + i / Z::WARPS % Z::DEPTH], (i / Z::WARPS / Z::DEPTH) & 1, p.status);
             return;
           }
@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(RaSize<HD, ROWS>::THREADS, 1)
             page_ok[st] = ok;
             unsigned char* dst = ring + (size_t)st * 2 * Z::TILE;
             mbar_expect_tx(&full[st], 2 * Z::TILE);
-            const int row = (page * p.c.Hkv + c.kvh) * PAGE + x % Z::STEPS * Z::TOK;
+            const int row = (page * p.c.Hkv + c.kvh) * PAGE;
 #pragma unroll
             for (int h = 0; h < HD / 64; ++h) {
               tma_load_2d(dst + h * Z::HALF, &kmap, h * 64, row, &full[st]);
@@ -180,11 +180,11 @@ __global__ void __launch_bounds__(RaSize<HD, ROWS>::THREADS, 1)
       for (int k = 0; k < KS; ++k) o[nb][k][0] = o[nb][k][1] = o[nb][k][2] = o[nb][k][3] = 0.f;
     }
 
-    const int len = (c.tile1 - c.tile0) * Z::STEPS;
+    const int len = c.tile1 - c.tile0;
 #pragma unroll 1
     for (int x = (warp - it % Z::WARPS + Z::WARPS) % Z::WARPS; x < len; x += Z::WARPS) {
       const int use = (it + x) / Z::WARPS, st = warp * Z::DEPTH + use % Z::DEPTH;
-      const int tok0 = c.tile0 * PAGE + x * Z::TOK;  // first token of the step
+      const int tok0 = (c.tile0 + x) * PAGE;  // first token of the step
       alive = alive && __all_sync(0xffffffffu, mbar_wait(&full[st], (use / Z::DEPTH) & 1, p.status));
       if (!alive) break;
       const uint32_t kb = smem_u32(ring + (size_t)st * 2 * Z::TILE), vb = kb + Z::TILE;
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(RaSize<HD, ROWS>::THREADS, 1)
         }
       // ---- which tokens are seen; a step inside the context is seen whole by every row ----
       uint64_t bad = 0;  // drafted tokens of the step with values that are not finite
-      if (ok && tok0 + Z::TOK <= C) {
+      if (ok && tok0 + PAGE <= C) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(RaSize<HD, ROWS>::THREADS, 1)
         // A weight of zero must not meet a value that is not finite.  Rows of the page behind the sequence are cleared, and so
         // are drafted tokens' rows with such values, which are added below for the query rows that see them.
 #pragma unroll 1
-        for (int w = 0; w < Z::TOK / 32; ++w) {
+        for (int w = 0; w < PAGE / 32; ++w) {
           const int r = lane + 32 * w, tok = tok0 + r;
           bool drop = tok >= T || !ok;
           if (!drop && tok >= C) {
@@ -579,8 +579,8 @@ template <int HD, int ROWS>
 static void launch_rows(RowsDev d, const RowsArgs& a, cudaStream_t st) {
   using Z = RaSize<HD, ROWS>;
   CUtensorMap kmap, vmap;
-  if (!encode_pool_map(&kmap, a.kv.k_pool, a.shape, a.kv.num_pages, Z::TOK) ||
-      !encode_pool_map(&vmap, a.kv.v_pool, a.shape, a.kv.num_pages, Z::TOK))
+  if (!encode_pool_map(&kmap, a.kv.k_pool, a.shape, a.kv.num_pages, PAGE) ||
+      !encode_pool_map(&vmap, a.kv.v_pool, a.shape, a.kv.num_pages, PAGE))
     return;
   // fewer CTAs where the caller's space for partial results is short
   const int rows = std::min(ROWS, d.c.max_nodes * d.c.G);
