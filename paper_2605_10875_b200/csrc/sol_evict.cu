@@ -264,7 +264,9 @@ __global__ void __launch_bounds__((2 * READERS + 2) * 32) evict_move_kernel(cons
   pdl_wait();
   const int chunks = (e.k + 31) / 32;
   const int pieces = bytes / 16, half = keys ? pieces / 2 : pieces;  // of a row's slab; those of its first half
-  const int shift = 31 - __clz(pieces);
+  // A lane copies piece `q` of every (32 / pieces)-th row from row r0 on
+  const int q = lane & (pieces - 1), r0 = lane / pieces, r_step = 32 / pieces, at_q = q < half ? q * 16 : ROW / 2 + (q - half) * 16;
+  const int f_shift = 31 - __clz(F);
   bool alive = true;
   auto wait = [&](uint64_t* bar, uint32_t parity) { alive = alive && __all_sync(0xffffffffu, mbar_wait(bar, parity, p.status)); };
 
@@ -338,17 +340,17 @@ __global__ void __launch_bounds__((2 * READERS + 2) * 32) evict_move_kernel(cons
       s.back[lane] = back;
       __syncwarp();
       const uint32_t data = smem_u32(s.data);
-#pragma unroll 8
-      for (int t = lane; t < 2 * bytes; t += 32) {
-        const int r = t >> shift, q = t - (r << shift);
-        const unsigned char* from = s.src[r];
-        if (from) em_copy16(data + t * 16, from + (q < half ? q * 16 : ROW / 2 + (q - half) * 16));
+#pragma unroll 4
+      for (int x = 0; x < pieces; ++x) {
+        const unsigned char* from = s.src[r0 + x * r_step];
+        if (from) em_copy16(data + (lane + 32 * x) * 16, from + at_q);
       }
       if (rope) {
         const int low = __reduce_min_sync(0xffffffffu, i < 0 ? 0x7fffffff : back >> 6), top = __reduce_max_sync(0xffffffffu, back >> 6);
         const bool fits = top - low < EM_FAR;
         if (fits)
-          for (int x = lane; x < (top - low + 1) * F; x += 32) enter(s.far + x / F * 2 * F, x % F, (low + x / F) * 64);
+          for (int x = lane; x < (top - low + 1) << f_shift; x += 32)
+            enter(s.far + (x >> f_shift) * 2 * F, x & (F - 1), (low + (x >> f_shift)) * 64);
         if (lane == 0) far0[st] = fits ? low : -1;
       }
       asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&full[st])) : "memory");
@@ -363,8 +365,9 @@ __global__ void __launch_bounds__((2 * READERS + 2) * 32) evict_move_kernel(cons
     return;
   }
 
-  // ---- a warp writes a chunk when it and all before it have arrived ----
+  // ---- a warp writes a chunk when it and all before it have arrived; of rotated keys a lane has piece f0 and the one half a row on ----
   int st = warp, phase = 0;
+  const int f0 = lane & (half - 1), f_r0 = lane / half, f_step = 32 / half;
 #pragma unroll 1
   for (int c = warp; c < chunks; c += WRITERS) {
     wait_arrived(c + 1);
@@ -374,15 +377,14 @@ __global__ void __launch_bounds__((2 * READERS + 2) * 32) evict_move_kernel(cons
     const uint4* data = reinterpret_cast<const uint4*>(s.data);
     if (!rope) {
 #pragma unroll 4
-      for (int t = lane; t < 2 * bytes; t += 32) {
-        const int r = t >> shift, q = t - (r << shift);
-        unsigned char* to = s.dst[r];
-        if (to) *reinterpret_cast<uint4*>(to + (q < half ? q * 16 : ROW / 2 + (q - half) * 16)) = data[t];
+      for (int x = 0; x < pieces; ++x) {
+        unsigned char* to = s.dst[r0 + x * r_step];
+        if (to) *reinterpret_cast<uint4*>(to + at_q) = data[lane + 32 * x];
       }
     } else {
-      const int f0 = lane % half, low = far0[st];
+      const int low = far0[st];
 #pragma unroll 2
-      for (int r = lane / half; r < 32; r += 32 / half) {
+      for (int r = f_r0; r < 32; r += f_step) {
         uint4* dst = reinterpret_cast<uint4*>(s.dst[r]);
         if (dst == nullptr) continue;
         const int back = s.back[r];
