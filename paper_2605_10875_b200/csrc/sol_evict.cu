@@ -174,10 +174,11 @@ __device__ __forceinline__ float2 turn_back(uint32_t back, uint2 speed) {
 // moves back never falls from one row to the next and hardly changes within a chunk, so its angle is put together from two tables
 // in shared memory, of 0 .. 63 positions and of the chunk's few multiples of 64 (an angle from the polynomials for every pair takes
 // three times the instructions); chunks that span more have their angles from the polynomials.
-// Bound by HBM and the writers' instructions for batches (half of 24 ragged caches, 1.1 GB: 221 us), by the time of a chunk times
-// the chunks of the longest sequence otherwise (half of 30000 tokens: 87 us).  Dropped: rows read into registers, between barriers,
-// 4 us a round, 317 us for the first; bulk copies of single rows, 25 to 40 ns each, 1447 us; every writer asking for every chunk
-// itself, 250 ns a chunk, 33 us where it is now 26; seven readers for a CTA that has an SM to itself, 121 us for the second.
+// Bound by HBM and the time from a chunk's request to its write for batches (half of 24 ragged caches, 1.1 GB: 213 us), by that time
+// and the chunks of the longest sequence otherwise (half of 30000 tokens: 81 us).  Dropped: rows read into registers, between
+// barriers, 4 us a round, 317 us for the first; bulk copies of single rows, 25 to 40 ns each, 1447 us; every writer asking for every
+// chunk itself, 250 ns a chunk, a quarter of 16 sequences of 4096 33 us where it is now 26; seven readers for a CTA that has an SM to
+// itself, 121 us for the second; rotated keys' pieces without their swap, 218 us for the first.
 constexpr int EM_FEW = 7, EM_MANY = 15;  // warps that read: where two CTAs share an SM, where one has it to itself
 constexpr uint32_t EM_POLLS = 1u << 22;  // some tenths of a second
 constexpr int EM_FAR = 4;          // multiples of 64 positions in a chunk's table
@@ -267,6 +268,8 @@ __global__ void __launch_bounds__((2 * READERS + 2) * 32) evict_move_kernel(cons
   // A lane copies piece `q` of every (32 / pieces)-th row from row r0 on
   const int q = lane & (pieces - 1), r0 = lane / pieces, r_step = 32 / pieces, at_q = q < half ? q * 16 : ROW / 2 + (q - half) * 16;
   const int f_shift = 31 - __clz(F);
+  // Where rotated keys' pieces lie: the halves of rows that a warp reads at once change places, so that they lie in different banks
+  auto swap = [&](int r) { return rope ? (r * half >> 2 & 1) * half : 0; };
   bool alive = true;
   auto wait = [&](uint64_t* bar, uint32_t parity) { alive = alive && __all_sync(0xffffffffu, mbar_wait(bar, parity, p.status)); };
 
@@ -312,6 +315,7 @@ __global__ void __launch_bounds__((2 * READERS + 2) * 32) evict_move_kernel(cons
       const int j = c * 32 + lane;
       next = j < e.k ? kept[j] : -1;
     };
+    const int to_q = lane ^ swap(r0);
     int c = warp - WRITERS, st = c, phase = 1;  // phase: of the stage's `empty`; the first use waits for none
     look(c);
 #pragma unroll 1
@@ -343,7 +347,7 @@ __global__ void __launch_bounds__((2 * READERS + 2) * 32) evict_move_kernel(cons
 #pragma unroll 4
       for (int x = 0; x < pieces; ++x) {
         const unsigned char* from = s.src[r0 + x * r_step];
-        if (from) em_copy16(data + (lane + 32 * x) * 16, from + at_q);
+        if (from) em_copy16(data + (to_q + 32 * x) * 16, from + at_q);
       }
       if (rope) {
         const int low = __reduce_min_sync(0xffffffffu, i < 0 ? 0x7fffffff : back >> 6), top = __reduce_max_sync(0xffffffffu, back >> 6);
@@ -367,7 +371,7 @@ __global__ void __launch_bounds__((2 * READERS + 2) * 32) evict_move_kernel(cons
 
   // ---- a warp writes a chunk when it and all before it have arrived; of rotated keys a lane has piece f0 and the one half a row on ----
   int st = warp, phase = 0;
-  const int f0 = lane & (half - 1), f_r0 = lane / half, f_step = 32 / half;
+  const int f0 = lane & (half - 1), f_r0 = lane / half, f_step = 32 / half, f_at = (f_r0 * pieces + f0) ^ swap(f_r0);
 #pragma unroll 1
   for (int c = warp; c < chunks; c += WRITERS) {
     wait_arrived(c + 1);
@@ -388,7 +392,8 @@ __global__ void __launch_bounds__((2 * READERS + 2) * 32) evict_move_kernel(cons
         uint4* dst = reinterpret_cast<uint4*>(s.dst[r]);
         if (dst == nullptr) continue;
         const int back = s.back[r];
-        const uint4 lo = data[r * pieces + f0], hi = data[r * pieces + half + f0];
+        const int at = f_at + (r - f_r0) * pieces;
+        const uint4 lo = data[at], hi = data[at ^ half];
         const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, h[4] = {hi.x, hi.y, hi.z, hi.w};
         uint32_t new_l[4], new_h[4];
         const float *a = near + (back & 63) * 2 * F + f0 * 4, *w = s.far + ((back >> 6) - max(low, 0)) * 2 * F + f0 * 4;
