@@ -360,7 +360,8 @@ sol_status_t sol_tree_commit(const sol_shape_t *shape, int32_t n_layers, const s
  * Dense decode attention of one query token per sequence (the newest, seq_lens counts it) over its whole cache, and
  *   weights[b][h][t] = decay * weights[b][h][t] + sum over the query heads of kv-head h of their softmax weight on token t
  * for every token t of the sequence; the newest token's entry is set to this step's sum.  Entries behind a sequence are left
- * as they were.  An empty sequence gets zeros.  Keep-rates, sinks, windows and the page selection do not act here.
+ * as they were.  An empty sequence gets zeros.  A length beyond the page table counts as its end, a negative one as zero, here
+ * and below.  Keep-rates, sinks, windows and the page selection do not act here.
  *   q_bf16, out_bf16 [B][n_q][head_dim]; weights float32 [B][n_kv][max_pages_per_seq * page_size]; 0 <= decay <= 1;
  *   ws: sol_workspace_bytes.  At most 256 kv-heads. */
 sol_status_t sol_weighted_decode_attn(const sol_shape_t *shape, const void *q_bf16, const sol_kv_t *kv, int32_t B, float decay,

@@ -309,6 +309,26 @@ def test_evict_captured_and_replayed_with_other_budgets():
         c.check(budgets)
 
 
+def test_lengths_out_of_range_count_as_the_nearest_in_range():
+    """A length beyond the page table is the table's end, a negative one is zero: the same bits as with those lengths."""
+    for wrong, right in (([1000, -3], [128, 0]), ([2**31 - 1, 128], [128, 128])):
+        a, b = Weighted("g4", [128, 128], seed=30, decay=0.5), Weighted("g4", [128, 128], seed=30, decay=0.5)
+        a.kv.seq_lens.copy_(torch.tensor(wrong, dtype=torch.int32))
+        b.kv.seq_lens.copy_(H.dev_i32(right))
+        a.launch()
+        b.launch()
+        assert torch.equal(a.out.view(torch.int16), b.out.view(torch.int16))
+        assert torch.equal(a.weights.view(torch.int32), b.weights.view(torch.int32))
+        c, d = Evict("g4", [128, 128], [60, 50], seed=31), Evict("g4", [128, 128], [60, 50], seed=31)
+        c.kv.seq_lens.copy_(torch.tensor(wrong, dtype=torch.int32))
+        d.kv.seq_lens.copy_(H.dev_i32(right))
+        c.launch()
+        d.launch()
+        assert torch.equal(c.dst_lens, d.dst_lens) and torch.equal(c.kept, d.kept) and torch.equal(c.dst_w, d.dst_w)
+        assert torch.equal(c.kv.k_pool.view(torch.int16), d.kv.k_pool.view(torch.int16))
+        assert c.ws.status()[0] == 0 and a.ws.status()[0] == 0
+
+
 def test_a_serving_loop_with_a_tree_and_a_budget():
     """A drafted tree is attended, accepted and committed; the weights of the next steps are kept; the cache is cut to a budget in
     place; the decode layer goes on with it.  Every stage against the oracle on what the stage really saw."""
