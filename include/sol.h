@@ -311,8 +311,10 @@ sol_status_t sol_kv_refresh(const sol_shape_t *shape, int32_t n_layers, const so
  *
  * The drafted nodes of sequence b are the last n_nodes[b] tokens of its cache: slots T_b - n_nodes[b] .. T_b - 1 hold
  * their keys and values in node order, seq_lens counts them, the tokens before them are the committed context.
- * At most 64 nodes; trees of a batch may differ, also in size.  A count outside 0 .. max_nodes, or above the
- * sequence's length, raises the bad-action bit of the device status word and is clamped. */
+ * At most 64 nodes; trees of a batch may differ, also in size.  A node count counts as the nearest one in 0 .. max_nodes that
+ * is not above the sequence's length, a length beyond the page table as its end, a negative one as zero.  sol_tree_attn and
+ * sol_tree_commit raise the bad-action bit of the device status word for them; sol_tree_build and sol_tree_accept, which have
+ * no status word and know no lengths, do not report. */
 #define SOL_MAX_TREE_NODES 64
 typedef struct sol_tree {
   int32_t max_nodes;      /* 1..64: rows per sequence of every [B][max_nodes] array */
@@ -349,7 +351,8 @@ sol_status_t sol_tree_accept(int32_t B, int32_t max_nodes, const int32_t *n_node
                              int32_t *next_token, sol_stream_t stream);
 /* Commits a path in all layers: the keys and values of its j-th node move to slot T_b - n_nodes[b] + j, in place; the other
  * nodes' slots are then free.  (A node of depth j was rotated for that position.)  The path must ascend; it ends at the
- * first entry that does not, or that is no node, which raises the bad-action bit.
+ * first entry that does not, or that is no node, which raises the bad-action bit, and so does a path_len outside
+ * 0 .. n_nodes[b], which counts as the nearest in range.
  *   kvs: HOST array of n_layers structs; tree: n_nodes and max_nodes (the mask may be NULL); new_lens [B] out, optional:
  *   the lengths of kvs[0] afterwards; it must not overlap any seq_lens, n_nodes or path_len; ws: an initialised workspace of
  *   any size (its status words).  The pages that hold the drafted nodes must belong to their sequence alone. */

@@ -124,11 +124,12 @@ __global__ void __launch_bounds__(COMMIT_THREADS) tree_commit_kernel(const Commi
   const sol_kv_t& kv = p.kv[layer];
   pdl_wait();
   pdl_trigger();
+  // counts out of range count as the nearest in range, as they do in the attention
   const int room = kv.max_pages_per_seq * PAGE;
-  const int T = kv.seq_lens[b];
-  int n = p.n_nodes[b], count = p.path_len[b];
-  const bool fits = T <= room && n >= 0 && n <= p.max_nodes && n <= T && count >= 0 && count <= n;
-  if (!fits) n = count = 0;
+  const int len = kv.seq_lens[b], nodes = p.n_nodes[b], steps = p.path_len[b];
+  const int T = min(max(len, 0), room), n = min(min(max(nodes, 0), p.max_nodes), T);
+  int count = min(max(steps, 0), n);
+  const bool fits = T == len && n == nodes && count == steps;
   if (tid < 32) {  // the path as far as it ascends within the tree
     bool ok[2];
 #pragma unroll
@@ -145,7 +146,7 @@ __global__ void __launch_bounds__(COMMIT_THREADS) tree_commit_kernel(const Commi
       const int run = ~good ? __ffsll((long long)~good) - 1 : 64;
       if (!fits || run < count) atomicOr(p.status + ST_ERR, ERR_BAD_ACTION);
       s_count = min(run, count);
-      if (layer == 0 && blockIdx.x == 0 && p.new_lens) p.new_lens[b] = (fits ? T - n : T) + s_count;
+      if (layer == 0 && blockIdx.x == 0 && p.new_lens) p.new_lens[b] = T - n + s_count;
     }
   }
   __syncthreads();
