@@ -107,6 +107,7 @@ __global__ void __launch_bounds__(TB_WARPS * 32) tree_accept_kernel(int B, int m
 struct CommitDev {
   sol_kv_t kv[COMMIT_LAYERS];
   int Hkv, hd, max_nodes;
+  int quest;  // tokens of a Quest page; 0: no extrema
   const int32_t* n_nodes;
   const int32_t* path;
   const int32_t* path_len;
@@ -116,7 +117,10 @@ struct CommitDev {
 
 // A CTA moves the accepted rows of a (layer, sequence, group of heads): thread = (head, K or V, 16-byte piece of a row), which
 // takes its piece of every row in the path's order, eight in flight.  In place: row j of the path goes to slot j, the path
-// ascends, so slot j is no later row's source (path[j'] >= j' > j), and no other thread touches the piece.
+// ascends, so slot j is no later row's source (path[j'] >= j' > j), and no other thread touches the piece.  With Quest pages the
+// thread then takes its eight dimensions' extrema of every block that drafted tokens lay in, over the tokens that are left: what
+// a decode step renews is the newest token's block alone.  (16 layers of 64 sequences,
+// 8 of 64 nodes accepted: 16 us; with blocks of 4 tokens 20.)
 constexpr int COMMIT_THREADS = 128;
 __global__ void __launch_bounds__(COMMIT_THREADS) tree_commit_kernel(const CommitDev p) {
   __shared__ int s_path[64], s_count;
@@ -185,6 +189,38 @@ __global__ void __launch_bounds__(COMMIT_THREADS) tree_commit_kernel(const Commi
     for (int u = 0; u < 8; ++u)
       if (dst[u]) *dst[u] = v[u];
   }
+  if (p.quest == 0 || kv.quest_meta == nullptr || n == 0 || i >= p.Hkv * ppr) return;
+  const int end = first + count;
+#pragma unroll 1
+  for (int t0 = first / p.quest * p.quest; t0 < end; t0 += p.quest) {
+    const uint4* rows = row(t0);
+    if (rows == nullptr) continue;
+    float top[8], low[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      top[e] = -INFINITY;
+      low[e] = INFINITY;
+    }
+#pragma unroll 4
+    for (int j = 0; j < min(p.quest, end - t0); ++j) {
+      const uint4 v = rows[(size_t)j * ppr];
+      const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float k = e & 1 ? bf16_hi(x[e >> 1]) : bf16_lo(x[e >> 1]);
+        top[e] = fmaxf(top[e], k);
+        low[e] = fminf(low[e], k);
+      }
+    }
+    const int page = table[t0 / PAGE];
+    uint32_t* meta = static_cast<uint32_t*>(kv.quest_meta) +
+                     ((((size_t)page * p.Hkv + kvh) * (PAGE / p.quest)) + t0 % PAGE / p.quest) * p.hd + piece * 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      meta[e] = pack_bf16(top[2 * e], top[2 * e + 1]);
+      meta[p.hd / 2 + e] = pack_bf16(-low[2 * e], -low[2 * e + 1]);
+    }
+  }
 }
 
 void launch_tree_build(int B, int max_nodes, const int32_t* n_nodes, const int32_t* parents, uint64_t* mask, int32_t* depth,
@@ -210,6 +246,7 @@ void launch_tree_commit(const sol_shape_t& sh, int n_layers, const sol_kv_t* kvs
     d.Hkv = sh.n_kv_heads;
     d.hd = sh.head_dim;
     d.max_nodes = tree.max_nodes;
+    d.quest = sh.token_select == SOL_SELECT_QUEST_PAGES ? sh.quest_page_size : 0;
     d.n_nodes = tree.n_nodes;
     d.path = path;
     d.path_len = path_len;
