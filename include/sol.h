@@ -354,8 +354,8 @@ sol_status_t sol_tree_accept(int32_t B, int32_t max_nodes, const int32_t *n_node
  * first entry that does not, or that is no node, which raises the bad-action bit, and so does a path_len outside
  * 0 .. n_nodes[b], which counts as the nearest in range.
  *   kvs: HOST array of n_layers structs; tree: n_nodes and max_nodes (the mask may be NULL); new_lens [B] out, optional:
- *   the lengths of kvs[0] afterwards; it must not overlap any seq_lens, n_nodes or path_len; ws: an initialised workspace of
- *   any size (its status words).  The pages that hold the drafted nodes must belong to their sequence alone.
+ *   the lengths of kvs[0] afterwards; it must not overlap any seq_lens, n_nodes, path or path_len; ws: an initialised workspace
+ *   of any size (its status words).  The pages that hold the drafted nodes must belong to their sequence alone.
  * With SOL_SELECT_QUEST_PAGES the extrema of every block that drafted nodes lay in are renewed over the tokens that stay, in
  * every layer that has a quest_meta. */
 sol_status_t sol_tree_commit(const sol_shape_t *shape, int32_t n_layers, const sol_kv_t *kvs, const sol_tree_t *tree, int32_t B,

@@ -794,10 +794,10 @@ static bool cache_size_ok(const sol_shape_t* s, const sol_kv_t* kv) {
 }
 static bool tree_ok(const sol_tree_t* t) { return t && t->n_nodes && t->mask && t->max_nodes >= 1; }
 static bool aligned8(const void* a) { return (reinterpret_cast<uintptr_t>(a) & 7) == 0; }
-// Do B int32 at a share any with those at b?  (An output that other CTAs of the call still read as an input.)
-static bool share_ints(const void* a, const void* b, int B) {
+// Do n int32 at a share any with the m at b?  (An output that other CTAs of the call still read as an input.)
+static bool share_ints(const void* a, size_t n, const void* b, size_t m) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return a && b && x < y + (size_t)B * 4 && y < x + (size_t)B * 4;
+  return a && b && x < y + m * 4 && y < x + n * 4;
 }
 
 // Which kernel takes a tree: a block of 16 query rows goes through mma.sync, more rows through tcgen05.
@@ -855,9 +855,11 @@ sol_status_t sol_tree_commit(const sol_shape_t* shape, int32_t n_layers, const s
                              const int32_t* path, const int32_t* path_len, int32_t* new_lens, void* ws, sol_stream_t stream) {
   if (!shape || n_layers < 1 || !kvs || !tree || !tree->n_nodes || tree->max_nodes < 1 || !path || !path_len || !ws || B < 0)
     return SOL_ERR_INVALID_ARG;
-  if (!aligned16(ws) || share_ints(new_lens, tree->n_nodes, B) || share_ints(new_lens, path_len, B)) return SOL_ERR_INVALID_ARG;
+  if (!aligned16(ws) || share_ints(new_lens, B, tree->n_nodes, B) || share_ints(new_lens, B, path_len, B) ||
+      share_ints(new_lens, B, path, (size_t)B * tree->max_nodes))
+    return SOL_ERR_INVALID_ARG;
   for (int l = 0; l < n_layers; ++l)
-    if (!kv_ok(&kvs[l]) || !aligned16(kvs[l].k_pool) || !aligned16(kvs[l].v_pool) || share_ints(new_lens, kvs[l].seq_lens, B))
+    if (!kv_ok(&kvs[l]) || !aligned16(kvs[l].k_pool) || !aligned16(kvs[l].v_pool) || share_ints(new_lens, B, kvs[l].seq_lens, B))
       return SOL_ERR_INVALID_ARG;
   if (!shape_ok(shape) || B > 128 || tree->max_nodes > MAX_TREE_NODES) return SOL_ERR_UNSUPPORTED;
   for (int l = 0; l < n_layers; ++l)
@@ -895,8 +897,8 @@ sol_status_t sol_kv_evict(const sol_shape_t* shape, const sol_kv_t* kv, int32_t 
                           size_t ws_bytes, sol_stream_t stream) {
   if (!shape || !kv_ok(kv) || !budgets || !weights || !dst_table || !dst_weights || !dst_lens || !ws || B < 0)
     return SOL_ERR_INVALID_ARG;
-  if (!aligned16(kv->k_pool) || !aligned16(kv->v_pool) || !aligned16(ws) || share_ints(dst_lens, kv->seq_lens, B) ||
-      share_ints(dst_lens, budgets, B))
+  if (!aligned16(kv->k_pool) || !aligned16(kv->v_pool) || !aligned16(ws) || share_ints(dst_lens, B, kv->seq_lens, B) ||
+      share_ints(dst_lens, B, budgets, B))
     return SOL_ERR_INVALID_ARG;
   if (!shape_ok(shape) || B > 128 || !cache_size_ok(shape, kv)) return SOL_ERR_UNSUPPORTED;
   if (B == 0) return SOL_OK;

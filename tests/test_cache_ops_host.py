@@ -124,6 +124,17 @@ def test_outputs_that_share_an_input_and_misaligned_words_are_refused():
                (I, lambda: sol.tree_attn(_shape(), FAKE, _kv(), sol.make_tree(8, FAKE, FAKE + 4), 2, FAKE, FAKE, BIG, check=False))])
 
 
+def test_new_lengths_over_the_path_are_refused():
+    """Every layer's CTAs read the path while the first layer's write the lengths."""
+    def commit(lens, path=0x5000, B=4, N=8):
+        kv = _kv(seq_lens=0x2000)
+        return lambda: sol.tree_commit(_shape(), [kv], sol.make_tree(N, 0x3000), B, path, 0x4000, lens, FAKE, check=False)
+
+    I = sol.SOL_ERR_INVALID_ARG
+    _refusals([(I, commit(0x5000)), (I, commit(0x5000 + 31 * 4)), (I, commit(0x5000 - 12)), (I, commit(0x5040, B=1, N=64)),
+               (sol.SOL_OK, commit(0x5000, B=0))])
+
+
 # ---- pins of the oracle --------------------------------------------------------------------------
 def _cache(lens, seed=0, theta=0.0):
     cfg = dict(synth.WORKLOADS["tiny"], shuffle_pages=True)
