@@ -384,10 +384,31 @@ sol_status_t sol_weighted_decode_attn(const sol_shape_t *shape, const void *q_bf
  * the pages then must belong to their sequence alone.  Otherwise the destinations must not overlap each other or what any
  * sequence of the batch still reads.  A row whose old or new page is out of range is left where it is and raises the status
  * bit.  The Quest extrema are not updated:
- * call sol_quest_build_meta afterwards.  ws: sol_workspace_bytes.  At most 256 kv-heads. */
+ * call sol_quest_build_meta afterwards.  ws: sol_workspace_bytes.  At most 256 kv-heads.
+ * Every call rounds the keys that it moves once more.  Over few large evictions that is little, but many small moves do not add up:
+ * a pair of elements that turns by less than half a bf16 step is rounded back to where it was.  (Normal keys, rope_theta 500000,
+ * 1000 positions in all, relative error by L2 norm: one move 0.002, 10 moves 0.008, 100 moves 0.05, 1000 moves 0.4.)  A cache out
+ * of which a few tokens go at a time is for sol_kv_evict_tracked. */
 sol_status_t sol_kv_evict(const sol_shape_t *shape, const sol_kv_t *kv, int32_t B, const int32_t *budgets, const float *weights,
                           const int32_t *dst_table, float *dst_weights, int32_t *dst_lens, int32_t *kept_idx, void *ws,
                           size_t ws_bytes, sol_stream_t stream);
+/* The same for a cache that is evicted from again and again: keys are rotated from what they were before they were first moved, by
+ * the whole distance, and rounded once, however many calls it took.
+ *   k_pool: as large as kv->k_pool and with the same pages: the first form of every key that has been moved (the call writes it, and
+ *   reads no other rows of it); it must not overlap the cache's pools.
+ *   moved int32 [B][n_kv][max_pages_per_seq * page_size]: how far the key in a slot has been moved in all, 0 for one that never was.
+ *   dst_moved: the same for the new slots, zeros behind them up to the row's end; it may be moved, and must not overlap it otherwise.
+ * A sequence begins with zeros in moved.  Keys that are appended to it then need nothing done; who writes a new key into a slot whose
+ * entry is not 0 (sol_kv_refresh) sets it to 0.  shape->rope_theta must be above 0: without it keys are not rounded. */
+typedef struct sol_key_origin {
+  void *k_pool;
+  const int32_t *moved;
+  int32_t *dst_moved;
+} sol_key_origin_t;
+sol_status_t sol_kv_evict_tracked(const sol_shape_t *shape, const sol_kv_t *kv, int32_t B, const int32_t *budgets,
+                                  const float *weights, const int32_t *dst_table, float *dst_weights, int32_t *dst_lens,
+                                  int32_t *kept_idx, const sol_key_origin_t *origin, void *ws, size_t ws_bytes,
+                                  sol_stream_t stream);
 
 /* The same step for a caller whose per-step data lives on the HOST: h_in,
  * the three action arrays, seq_lens and h_out are host pointers (pinned

@@ -27,7 +27,7 @@ EXPORTS = [
     "sol_sparse_decode_attn", "sol_sparse_decode_attn_static", "sol_pruned_swiglu_mlp", "sol_decode_layer", "sol_decode_step",
     "sol_decode_step_traced", "sol_kv_refresh", "sol_decode_step_host", "sol_read_device_status", "sol_selftest_wait_timeout", "sol_timing_enable", "sol_timing_collect",
     "sol_launch_count", "sol_tree_workspace_bytes", "sol_tree_build", "sol_tree_attn", "sol_tree_accept", "sol_tree_commit",
-    "sol_weighted_decode_attn", "sol_kv_evict",
+    "sol_weighted_decode_attn", "sol_kv_evict", "sol_kv_evict_tracked",
 ]
 
 
@@ -47,6 +47,10 @@ class SolKV(C.Structure):
 
 class SolTree(C.Structure):
     _fields_ = [("max_nodes", C.c_int32), ("n_nodes", C.c_void_p), ("mask", C.c_void_p)]
+
+
+class SolKeyOrigin(C.Structure):
+    _fields_ = [("k_pool", C.c_void_p), ("moved", C.c_void_p), ("dst_moved", C.c_void_p)]
 
 
 class SolLayerWeights(C.Structure):
@@ -142,6 +146,8 @@ def lib() -> C.CDLL:
         L.sol_weighted_decode_attn.argtypes = [C.POINTER(SolShape), P, C.POINTER(SolKV), I, C.c_float, P, P, P, S, P]
         L.sol_kv_evict.restype = I
         L.sol_kv_evict.argtypes = [C.POINTER(SolShape), C.POINTER(SolKV), I, P, P, P, P, P, P, P, S, P]
+        L.sol_kv_evict_tracked.restype = I
+        L.sol_kv_evict_tracked.argtypes = [C.POINTER(SolShape), C.POINTER(SolKV), I, P, P, P, P, P, P, C.POINTER(SolKeyOrigin), P, S, P]
         L.sol_timing_enable.restype = None
         L.sol_timing_enable.argtypes = [I]
         L.sol_timing_collect.restype = I
@@ -399,13 +405,23 @@ def weighted_decode_attn(shape, q_bf16, kv: SolKV, B: int, decay: float, weights
     return s
 
 
+def make_key_origin(k_pool, moved, dst_moved=None) -> SolKeyOrigin:
+    """What kv_evict tracks keys with: a second pool for their first form, and int32 [B][n_kv][slots], how far each was moved; in
+    place where there is no dst_moved."""
+    return SolKeyOrigin(_ptr(k_pool), _ptr(moved), _ptr(moved if dst_moved is None else dst_moved))
+
+
 def kv_evict(shape, kv: SolKV, B: int, budgets, weights, dst_table, dst_weights, dst_lens, kept_idx, ws, ws_bytes: int,
-             stream=None, check=True) -> int:
-    """Keeps the budget's tokens of largest weight per (sequence, kv-head); dst_table and dst_weights may be the cache's own."""
-    s = lib().sol_kv_evict(C.byref(shape), C.byref(kv), B, _ptr(budgets), _ptr(weights), _ptr(dst_table), _ptr(dst_weights),
-                           _ptr(dst_lens), _ptr(kept_idx), _ptr(ws), ws_bytes, _stream(stream))
+             stream=None, check=True, origin: Optional[SolKeyOrigin] = None) -> int:
+    """Keeps the budget's tokens of largest weight per (sequence, kv-head); dst_table and dst_weights may be the cache's own.
+    With an origin, keys are rounded once however often they are moved."""
+    head = (C.byref(shape), C.byref(kv), B, _ptr(budgets), _ptr(weights), _ptr(dst_table), _ptr(dst_weights), _ptr(dst_lens),
+            _ptr(kept_idx))
+    tail = (_ptr(ws), ws_bytes, _stream(stream))
+    name = "sol_kv_evict" if origin is None else "sol_kv_evict_tracked"
+    s = lib().sol_kv_evict(*head, *tail) if origin is None else lib().sol_kv_evict_tracked(*head, C.byref(origin), *tail)
     if check:
-        _check(s, "sol_kv_evict")
+        _check(s, name)
     return s
 
 

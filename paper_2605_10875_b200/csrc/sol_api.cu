@@ -892,9 +892,9 @@ sol_status_t sol_weighted_decode_attn(const sol_shape_t* shape, const void* q_bf
   return finish();
 }
 
-sol_status_t sol_kv_evict(const sol_shape_t* shape, const sol_kv_t* kv, int32_t B, const int32_t* budgets, const float* weights,
-                          const int32_t* dst_table, float* dst_weights, int32_t* dst_lens, int32_t* kept_idx, void* ws,
-                          size_t ws_bytes, sol_stream_t stream) {
+static sol_status_t evict(const sol_shape_t* shape, const sol_kv_t* kv, int32_t B, const int32_t* budgets, const float* weights,
+                          const int32_t* dst_table, float* dst_weights, int32_t* dst_lens, int32_t* kept_idx,
+                          const sol_key_origin_t* origin, void* ws, size_t ws_bytes, sol_stream_t stream) {
   if (!shape || !kv_ok(kv) || !budgets || !weights || !dst_table || !dst_weights || !dst_lens || !ws || B < 0)
     return SOL_ERR_INVALID_ARG;
   if (!aligned16(kv->k_pool) || !aligned16(kv->v_pool) || !aligned16(ws) || share_ints(dst_lens, B, kv->seq_lens, B) ||
@@ -909,9 +909,34 @@ sol_status_t sol_kv_evict(const sol_shape_t* shape, const sol_kv_t* kv, int32_t 
   a.shape = *shape; a.kv = *kv; a.B = B; a.budgets = budgets; a.weights = weights;
   a.dst_table = dst_table; a.dst_weights = dst_weights; a.dst_lens = dst_lens;
   a.kept_idx = kept_idx ? kept_idx : at<int32_t>(ws, L.attn.kept_idx);
+  if (origin) {
+    a.first_keys = origin->k_pool; a.moved = origin->moved; a.dst_moved = origin->dst_moved;
+  }
   a.status = at<int>(ws, L.status);
   launch_evict(a, (cudaStream_t)stream);
   return finish();
+}
+
+sol_status_t sol_kv_evict(const sol_shape_t* shape, const sol_kv_t* kv, int32_t B, const int32_t* budgets, const float* weights,
+                          const int32_t* dst_table, float* dst_weights, int32_t* dst_lens, int32_t* kept_idx, void* ws,
+                          size_t ws_bytes, sol_stream_t stream) {
+  return evict(shape, kv, B, budgets, weights, dst_table, dst_weights, dst_lens, kept_idx, nullptr, ws, ws_bytes, stream);
+}
+
+sol_status_t sol_kv_evict_tracked(const sol_shape_t* shape, const sol_kv_t* kv, int32_t B, const int32_t* budgets,
+                                  const float* weights, const int32_t* dst_table, float* dst_weights, int32_t* dst_lens,
+                                  int32_t* kept_idx, const sol_key_origin_t* origin, void* ws, size_t ws_bytes,
+                                  sol_stream_t stream) {
+  if (!shape || !kv_ok(kv) || !origin || !origin->k_pool || !origin->moved || !origin->dst_moved || !aligned16(origin->k_pool) || B < 0)
+    return SOL_ERR_INVALID_ARG;
+  if (!(shape->rope_theta > 0.f)) return SOL_ERR_INVALID_ARG;
+  if (!shape_ok(shape) || B > 128 || !cache_size_ok(shape, kv)) return SOL_ERR_UNSUPPORTED;
+  const size_t pool = (size_t)kv->num_pages * shape->n_kv_heads * PAGE * shape->head_dim / 2;  // in words
+  const size_t rows = (size_t)B * shape->n_kv_heads * kv->max_pages_per_seq * PAGE;
+  if (share_ints(origin->k_pool, pool, kv->k_pool, pool) || share_ints(origin->k_pool, pool, kv->v_pool, pool) ||
+      (origin->moved != origin->dst_moved && share_ints(origin->moved, rows, origin->dst_moved, rows)))
+    return SOL_ERR_INVALID_ARG;
+  return evict(shape, kv, B, budgets, weights, dst_table, dst_weights, dst_lens, kept_idx, origin, ws, ws_bytes, stream);
 }
 
 // The per-sequence actions and lengths of a step (at most 128 sequences) travel as kernel parameters:

@@ -5,6 +5,13 @@
 //   evict_move_kernel    rows of keys and values to their new slots.  A key moves from position i to position j <= i and is
 //                        rotated by j - i, so that slot t keeps a key at position t, which is where the decode step will put
 //                        its queries and the next key.
+//   evict_moved_kernel   with tracked origins: how far every kept key has been moved in all
+//
+// A key that is rotated where it lies is rounded to bf16 each time, and the roundings of many small turns do not cancel: a pair that
+// turns by less than half a step stays where it was.  (Keys off by 0.0017 after one move; 200 moves of one position 0.032, 1000 0.44.)
+// With tracked origins a key is rotated from what it was before its first move, by the whole distance, and rounded once.  That writes
+// every moved key twice and leaves its angles to the polynomials where neighbours have moved unequally far (half of 24 caches of 9000
+// 216 us, tracked 276; one token of 16 caches of 4097, head_dim 64, 69 us, tracked 92).
 #include <math.h>
 
 #include <algorithm>
@@ -225,7 +232,9 @@ __device__ __forceinline__ uint32_t em_pack(float lo, float hi) {
   return y;
 }
 
-template <int HD, int READERS>
+// TRACK: with tracked origins.  A key that has been moved before comes from its row of first_keys, and every key that moves leaves
+// there what it was, in the same order as the rows themselves: what is read later lies behind every slot written so far, in either pool.
+template <int HD, int READERS, bool TRACK>
 __global__ void __launch_bounds__((2 * READERS + 2) * 32) evict_move_kernel(const EvictArgs p, const MoveShape sh) {
   constexpr int WRITERS = READERS + 1, ORDER = WRITERS + READERS, THREADS = (ORDER + 1) * 32;
   constexpr int ROW = HD * 2;      // bytes of a row
@@ -238,6 +247,7 @@ __global__ void __launch_bounds__((2 * READERS + 2) * 32) evict_move_kernel(cons
   const int kvh = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int Hkv = p.shape.n_kv_heads, mp = p.kv.max_pages_per_seq;
   const bool keys = blockIdx.x < slabs, rope = keys && p.shape.rope_theta > 0.f;
+  const ptrdiff_t to_first = TRACK ? static_cast<unsigned char*>(p.first_keys) - static_cast<unsigned char*>(p.kv.k_pool) : 0;
   const int stages = keys ? sh.key_stages : sh.value_stages;
   const int slab = keys ? blockIdx.x : blockIdx.x - slabs;
   float* near = reinterpret_cast<float*>(em_smem);  // [64][2][F] cosines, sines
@@ -342,7 +352,8 @@ __global__ void __launch_bounds__((2 * READERS + 2) * 32) evict_move_kernel(cons
     for (; c < chunks; c += READERS) {
       const Stage s = stage(st);
       unsigned char *src = nullptr, *dst = nullptr;
-      const int i = next, j = c * 32 + lane, back = i < 0 ? 0 : i - j;
+      const int i = next, j = c * 32 + lane, before = TRACK && keys && i >= 0 ? p.moved[row + i] : 0;
+      const int back = i < 0 ? 0 : i - j + before;
       if (i >= 0) {
         const int from = table[i / PAGE], to = dst_table[j / PAGE];
         if ((unsigned)from >= (unsigned)p.kv.num_pages || (unsigned)to >= (unsigned)p.kv.num_pages) {
@@ -351,6 +362,7 @@ __global__ void __launch_bounds__((2 * READERS + 2) * 32) evict_move_kernel(cons
           src = pool + (((size_t)from * Hkv + kvh) * PAGE + i % PAGE) * ROW + first;
           dst = pool + (((size_t)to * Hkv + kvh) * PAGE + j % PAGE) * ROW + first;
           if (src == dst) src = dst = nullptr;  // it stays where it is
+          else if (TRACK && before) src += to_first;
         }
       }
       look(c + READERS);
@@ -444,6 +456,11 @@ __global__ void __launch_bounds__((2 * READERS + 2) * 32) evict_move_kernel(cons
         }
         dst[f0] = back ? make_uint4(new_l[0], new_l[1], new_l[2], new_l[3]) : lo;
         dst[f0 + ROW / 32] = back ? make_uint4(new_h[0], new_h[1], new_h[2], new_h[3]) : hi;
+        if (TRACK) {
+          uint4* first = reinterpret_cast<uint4*>(reinterpret_cast<unsigned char*>(dst) + to_first);
+          first[f0] = lo;
+          first[f0 + ROW / 32] = hi;
+        }
       }
     }
     __syncwarp();
@@ -456,7 +473,27 @@ __global__ void __launch_bounds__((2 * READERS + 2) * 32) evict_move_kernel(cons
   }
 }
 
-template <int HD>
+// How far the kept keys have been moved in all; none of what lies behind them has.  A CTA per (sequence, kv-head): in place the entries
+// of a chunk are read before any is written, and those of later chunks lie behind them (kept_idx[j] >= j).
+__global__ void __launch_bounds__(ES_THREADS) evict_moved_kernel(const EvictArgs p) {
+  pdl_trigger();
+  const int b = blockIdx.y, n = p.kv.max_pages_per_seq * PAGE, k = evict_plan(p, b).k;
+  const size_t row = ((size_t)b * p.shape.n_kv_heads + blockIdx.x) * n;
+  pdl_wait();
+#pragma unroll 1
+  for (int j0 = 0; j0 < n; j0 += ES_THREADS) {
+    const int j = j0 + threadIdx.x;
+    int far = 0;
+    if (j < k) {
+      const int i = p.kept_idx[row + j];
+      far = p.moved[row + i] + i - j;
+    }
+    __syncthreads();
+    if (j < n) p.dst_moved[row + j] = far;
+  }
+}
+
+template <int HD, bool TRACK>
 static void launch_move(const EvictArgs& a, cudaStream_t st) {
   const int Hkv = a.shape.n_kv_heads, rows = 2 * a.B * Hkv;
   MoveShape sh;
@@ -475,7 +512,7 @@ static void launch_move(const EvictArgs& a, cudaStream_t st) {
   sh.key_stages = std::min(EM_MAX_STAGES, (room - near) / em_stage_bytes(HD, sh.slabs, true));  // at least as many as readers, writers
   sh.value_stages = std::min(EM_MAX_STAGES, room / em_stage_bytes(HD, sh.slabs, false));
   const int smem = std::max(near + sh.key_stages * em_stage_bytes(HD, sh.slabs, true), sh.value_stages * em_stage_bytes(HD, sh.slabs, false));
-  const auto kernel = two ? evict_move_kernel<HD, EM_FEW> : evict_move_kernel<HD, EM_MANY>;
+  const auto kernel = two ? evict_move_kernel<HD, EM_FEW, TRACK> : evict_move_kernel<HD, EM_MANY, TRACK>;
   ensure_dynamic_smem(reinterpret_cast<const void*>(kernel), smem);
   SOL_LAUNCH("evict_move", kernel, dim3(2 * sh.slabs, Hkv, a.B), dim3((2 * (two ? EM_FEW : EM_MANY) + 2) * 32), smem, st, a, sh);
 }
@@ -485,8 +522,14 @@ void launch_evict(const EvictArgs& a, cudaStream_t st) {
   const int smem = per * ES_THREADS * 4;
   ensure_dynamic_smem(reinterpret_cast<const void*>(&evict_select_kernel), smem);
   SOL_LAUNCH("evict_select", evict_select_kernel, dim3(a.shape.n_kv_heads, a.B), dim3(ES_THREADS), smem, st, a);
-  if (a.shape.head_dim == 64) launch_move<64>(a, st);
-  else launch_move<128>(a, st);
+  if (a.first_keys) {
+    if (a.shape.head_dim == 64) launch_move<64, true>(a, st);
+    else launch_move<128, true>(a, st);
+    SOL_LAUNCH("evict_moved", evict_moved_kernel, dim3(a.shape.n_kv_heads, a.B), dim3(ES_THREADS), 0, st, a);
+  } else {
+    if (a.shape.head_dim == 64) launch_move<64, false>(a, st);
+    else launch_move<128, false>(a, st);
+  }
 }
 
 }  // namespace sol

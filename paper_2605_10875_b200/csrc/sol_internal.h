@@ -386,6 +386,9 @@ struct EvictArgs {
   float* dst_weights;          // as weights
   int32_t* dst_lens;           // [B]
   int32_t* kept_idx;           // [B][Hkv][max_pages * 64]
+  void* first_keys;            // optional: a pool like the keys', with the keys as they were before they were first moved
+  const int32_t* moved;        // ... [B][Hkv][max_pages * 64]: how far since then
+  int32_t* dst_moved;          // ... as moved
   int* status;
 };
 void launch_evict(const EvictArgs& a, cudaStream_t st);

@@ -135,6 +135,27 @@ def test_new_lengths_over_the_path_are_refused():
                (sol.SOL_OK, commit(0x5000, B=0))])
 
 
+def test_tracked_eviction_refuses():
+    """What sol_kv_evict refuses, an origin that is not whole, keys without rotation, pools and arrays that overlap."""
+    POOL = 32 * 2 * 64 * 64 * 2  # bytes of the cache's keys
+    ROWS = 2 * 2 * 8 * 64 * 4    # ... of `moved`
+    FAR = 1 << 30
+
+    def call(pool=FAR, moved=FAKE, dst=None, shape=None, kv=None, B=2, lens=0x2000, size=BIG):
+        origin = sol.make_key_origin(pool, moved, dst)
+        kv = kv or _kv(k_pool=0x100000, v_pool=0x100000 + POOL)
+        return lambda: sol.kv_evict(shape or _shape(rope_theta=10000.0), kv, B, FAKE, FAKE, FAKE, FAKE, lens, None, FAKE, size,
+                                    check=False, origin=origin)
+
+    I, U, Z = sol.SOL_ERR_INVALID_ARG, sol.SOL_ERR_UNSUPPORTED, sol.SOL_ERR_WORKSPACE_TOO_SMALL
+    _refusals([(I, call(pool=None)), (I, call(moved=None, dst=FAKE)), (I, call(pool=FAR + 8)), (I, call(shape=_shape())),
+               (I, call(pool=0x100000)), (I, call(pool=0x100000 + POOL - 16)), (I, call(pool=0x100000 - POOL + 16)),
+               (I, call(pool=0x100000 + 2 * POOL - 16)), (Z, call(pool=0x100000 + 2 * POOL, size=0)),
+               (I, call(dst=FAKE + ROWS - 4)), (Z, call(dst=FAKE + ROWS, size=0)), (Z, call(dst=FAKE, size=0)),
+               (I, call(lens=FAKE)), (I, call(B=-1)), (U, call(B=129)), (U, call(kv=_kv(max_pages_per_seq=769))), (sol.SOL_OK, call(B=0))]
+              + [(U, call(shape=_shape(rope_theta=10000.0, **s))) for s in BAD_SHAPES])
+
+
 # ---- pins of the oracle --------------------------------------------------------------------------
 def _cache(lens, seed=0, theta=0.0):
     cfg = dict(synth.WORKLOADS["tiny"], shuffle_pages=True)
