@@ -337,6 +337,7 @@ size_t sol_tree_workspace_bytes(const sol_shape_t *shape, int32_t max_batch, int
  * the page selection do not act here.  What a masked node's key and value hold, numbers or not, does not reach a row that
  * does not see it; neither do slots behind the sequence.  Tokens of a page whose number is out of range are skipped and
  * raise the status bit.  At most 256 kv-heads.
+ * A value that is infinite makes its element of every row that sees it infinite, NaN where NaN or the other infinity is seen too.
  * Scores, maxima and sums are float32; the weights are rounded to bf16 for the product with V.
  *   q_bf16 [B][max_nodes][n_q][head_dim] (already rotated); out_bf16 the same shape. */
 sol_status_t sol_tree_attn(const sol_shape_t *shape, const void *q_bf16, const sol_kv_t *kv, const sol_tree_t *tree, int32_t B,
@@ -366,7 +367,7 @@ sol_status_t sol_tree_commit(const sol_shape_t *shape, int32_t n_layers, const s
  *   weights[b][h][t] = decay * weights[b][h][t] + sum over the query heads of kv-head h of their softmax weight on token t
  * for every token t of the sequence; the newest token's entry is set to this step's sum.  Entries behind a sequence are left
  * as they were.  An empty sequence gets zeros.  A length beyond the page table counts as its end, a negative one as zero, here
- * and below.  Keep-rates, sinks, windows and the page selection do not act here.
+ * and below.  Infinite values as in sol_tree_attn.  Keep-rates, sinks, windows and the page selection do not act here.
  *   q_bf16, out_bf16 [B][n_q][head_dim]; weights float32 [B][n_kv][max_pages_per_seq * page_size]; 0 <= decay <= 1;
  *   ws: sol_workspace_bytes.  At most 256 kv-heads. */
 sol_status_t sol_weighted_decode_attn(const sol_shape_t *shape, const void *q_bf16, const sol_kv_t *kv, int32_t B, float decay,

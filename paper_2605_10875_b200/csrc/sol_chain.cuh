@@ -248,6 +248,66 @@ __device__ __forceinline__ void chain_describe(const ChainShape& c, const ChainP
   out[cta] = d;
 }
 
+// ---- sums that are no numbers ----
+// The value of a token that is infinite makes its column of every row that sees it infinite, or NaN where it meets NaN or the other
+// infinity.  The products do not keep to that: a weight that is zero in one of its parts, or in a copy of the row that leaves the
+// token to another copy, makes NaN of it.  So where a sum of numbers' weights is no number, the column is made out again from what the
+// values are.  Nothing but such sums pays for it.
+enum : int { VALUE_PLUS = 1, VALUE_MINUS = 2, VALUE_NAN = 4 };
+__device__ __forceinline__ int value_flag(uint32_t bf16) {
+  return (bf16 & 0x7f80u) != 0x7f80u ? 0 : bf16 & 0x7fu ? VALUE_NAN : bf16 & 0x8000u ? VALUE_MINUS : VALUE_PLUS;
+}
+__device__ __forceinline__ float flagged_sum(int flags, float was) {
+  return flags == 0 ? was : flags == VALUE_PLUS ? INFINITY : flags == VALUE_MINUS ? -INFINITY : NAN;
+}
+struct ValueRows {  // a (sequence, kv-head)'s
+  const uint16_t* pool;
+  const int32_t* table;
+  int num_pages, Hkv, kvh;
+  template <int HD>
+  __device__ __forceinline__ const uint16_t* row(int tok) const {  // nullptr: its page is out of range
+    const int page = table[tok / PAGE];
+    return (unsigned)page < (unsigned)num_pages ? pool + (((size_t)page * Hkv + kvh) * PAGE + tok % PAGE) * HD : nullptr;
+  }
+};
+__device__ __forceinline__ ValueRows value_rows(const sol_kv_t& kv, int Hkv, int b, int kvh) {
+  ValueRows v;
+  v.pool = static_cast<const uint16_t*>(kv.v_pool);
+  v.table = kv.page_table + (size_t)b * kv.max_pages_per_seq;
+  v.num_pages = kv.num_pages;
+  v.Hkv = Hkv;
+  v.kvh = kvh;
+  return v;
+}
+// What tokens [t0, t1) hold: a word of flags per column, cleared before, by thread `i` of n (a multiple of HD / 8).
+template <int HD>
+__device__ __noinline__ void value_flags(const ValueRows v, int t0, int t1, int i, int n, int* flags) {
+  constexpr int PPR = HD / 8;
+  uint32_t found = 0;  // three bits per column
+#pragma unroll 4
+  for (int t = t0 + i / PPR; t < t1; t += n / PPR) {
+    const uint16_t* row = v.row<HD>(t);
+    if (row == nullptr) continue;
+    const uint4 x = *reinterpret_cast<const uint4*>(row + i % PPR * 8);
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) found |= (uint32_t)value_flag(e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu) << (3 * e);
+  }
+  for (int e = 0; e < 8; ++e)
+    if ((found >> (3 * e)) & 7u) atomicOr(flags + i % PPR * 8 + e, (int)((found >> (3 * e)) & 7u));
+}
+// ... and of the nodes among [t0, t1) that a row sees, in one column.  C: slot of node 0.
+template <int HD>
+__device__ __forceinline__ int node_flags(const ValueRows& v, int t0, int t1, int C, uint64_t nodes, int col) {
+  int f = 0;
+  for (; nodes; nodes &= nodes - 1) {
+    const int t = C + __ffsll((long long)nodes) - 1;
+    const uint16_t* row = t >= t0 && t < t1 ? v.row<HD>(t) : nullptr;
+    if (row) f |= value_flag(row[col]);
+  }
+  return f;
+}
+
 // A row's merged maximum and 1 / (sum of the weights) (0 for a row that sees nothing), by the 16 lanes of half a warp.
 __device__ __forceinline__ float2 chain_merged_ml(const ChainParts& p, const ChainCut& cut, int row) {
   const int sub = threadIdx.x & 15, np = cut.pieces();
@@ -278,7 +338,7 @@ __device__ __forceinline__ void chain_merged_row(const ChainParts& p, const Chai
 #pragma unroll 4
   for (int i = 0; i < np; ++i) {
     const size_t at = (size_t)cut.slot(i) * p.rows + row;
-    const float f = exp2f(p.ml[at].x - ml.x) * inv;
+    const float f = fmaxf(exp2f(p.ml[at].x - ml.x), 1e-37f) * inv;  // above 0: sums may be infinite
 #pragma unroll
     for (int x = 0; x < V; ++x) {
       const float4 v = *reinterpret_cast<const float4*>(p.sums + at * HD + x * 64 + sub * 4);

@@ -68,6 +68,34 @@ __device__ __forceinline__ void ra_consumer_sync() {
   asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
 }
 
+// Rows of a piece with sums that are no numbers (`redo`: a bit per lane's row), by the warp that has stored them: bf16 to the output
+// or float32 to the partial results.
+template <int HD, int ROWS>
+__device__ __noinline__ void ra_redo(const ValueRows v, const uint64_t* mask, int G, int C, int t0, int t1, int row0, int redo, int* flags,
+                                     uint16_t* out, int Hq, float* part) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  for (int d = lane; d < HD; d += 32) flags[d] = 0;
+  __syncwarp();
+  value_flags<HD>(v, t0, min(t1, C), lane, 32, flags);
+  __syncwarp();
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    if (!((redo >> i) & 1)) continue;
+    const int r = (i >> 1) * 8 + 2 * t + (i & 1), node = (row0 + r) / G;
+    const uint64_t nodes = mask ? mask[node] : 1ull;  // (nodes that are not there lie behind t1)
+#pragma unroll 1
+    for (int d = g; d < HD; d += 8) {
+      uint16_t* o = out + ((size_t)node * Hq + (row0 + r - node * G)) * HD + d;
+      const float was = part ? part[r * HD + d] : bf2f(*o);
+      if (fabsf(was) < INFINITY) continue;
+      const float now = flagged_sum(flags[d] | node_flags<HD>(v, t0, t1, C, nodes, d), was);
+      if (part) part[r * HD + d] = now;
+      else *o = f2bf(now);
+    }
+  }
+  __syncwarp();
+}
+
 template <int HD, int ROWS>
 __global__ void __launch_bounds__(RaSize<HD, ROWS>::THREADS, 1)
     rows_attn_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const RowsDev p) {
@@ -79,6 +107,7 @@ __global__ void __launch_bounds__(RaSize<HD, ROWS>::THREADS, 1)
   __shared__ ChainPlan plan;
   __shared__ uint64_t full[Z::STAGES], empty[Z::STAGES];
   __shared__ int page_ok[Z::STAGES];
+  __shared__ int flags[HD];
   unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(ra_smem) + 1023) & ~(uintptr_t)1023);
   float* merge = reinterpret_cast<float*>(ring + Z::STAGES * 2 * Z::TILE);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -392,6 +421,7 @@ __global__ void __launch_bounds__(RaSize<HD, ROWS>::THREADS, 1)
     if (warp == 0) {
       const bool whole = c.whole();
       const size_t part = (size_t)(2 * blockIdx.x + (u > u0)) * p.part.rows;
+      int redo = 0;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         if (PACK) {  // high and low parts
@@ -425,8 +455,16 @@ __global__ void __launch_bounds__(RaSize<HD, ROWS>::THREADS, 1)
             }
             if (g == 0) p.part.ml[part + r] = make_float2(m[nb][e], sum);
           }
+          float none = 0.f;
+#pragma unroll
+          for (int k = 0; k < KS; ++k) none = fmaf(o[nb][k][e], 0.f, fmaf(o[nb][k][2 + e], 0.f, none));
+          if (none != 0.f && sum < INFINITY) redo |= 1 << (nb * 2 + e);  // (NaN differs from 0, and is not below infinity)
         }
       }
+      if (__any_sync(0xffffffffu, redo))
+        ra_redo<HD, ROWS>(value_rows(p.c.kv, p.c.Hkv, c.b, c.kvh), p.mask ? p.mask + (size_t)c.b * p.c.max_nodes : nullptr, G, C,
+                          c.tile0 * PAGE, min(T, c.tile1 * PAGE), row0, redo, flags,
+                          p.out + ((size_t)c.b * p.c.max_nodes * p.Hq + c.kvh * G) * HD, p.Hq, whole ? nullptr : p.part.sums + part * HD);
     }
     u = c.next;
   }

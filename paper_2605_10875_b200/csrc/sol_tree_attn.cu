@@ -393,6 +393,21 @@ __device__ __forceinline__ void tree_units_sync() {
   asm volatile("bar.sync 1, 256;" ::: "memory");
 }
 
+// ... and whether any thread says so
+__device__ __forceinline__ bool tree_units_any(bool mine) {
+  uint32_t y;
+  __syncwarp();
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "bar.red.or.pred q, 1, 256, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(y)
+      : "r"((uint32_t)mine)
+      : "memory");
+  return y != 0;
+}
+
 // Bits of the 32 tokens from `base` on that a row sees: the context, and its mask's nodes.
 __device__ __forceinline__ uint32_t tree_seen(int base, int C, uint64_t nodes) {
   const int ctx = C - base;
@@ -498,6 +513,45 @@ __device__ __noinline__ void tree_add_dirty(const TreeDev& p, int b, int kvh, in
     const float w = ta_exp2(fmaf(dot, p.scale_log2, m == -INFINITY ? 0.f : -m)) * f;
     for (int i = 0; i < TA_EX; ++i) ex[i * 256 + (me ^ (i >> 3 << 3))] += w * bf2f(v[i]);
   }
+}
+
+// Are a row's weights numbers?  (pad: lanes from one of its shares to the next)
+__device__ __forceinline__ bool tree_weights_ok(const float2* ml, int row, int pad) {
+  bool ok = true;
+  for (int i = row; i < 256; i += pad) ok = ok && ml[i].y < INFINITY;  // NaN is not
+  return ok;
+}
+
+// A piece with sums that are no numbers, by the units' 256 threads: each takes the elements that it has stored, eight a time.
+template <int HD>
+__device__ __noinline__ void tree_redo(const TreeDev& p, const TreePiece c, int pad, const float2* ml, int* flags, float* part) {
+  const int tid = threadIdx.x, G = p.c.G, t0 = c.tile0 * TA_TILE, t1 = min(c.seq.T, c.tile1 * TA_TILE);
+  const ValueRows v = value_rows(p.c.kv, p.c.Hkv, c.b, c.kvh);
+  if (tid < HD) flags[tid] = 0;
+  tree_units_sync();
+  value_flags<HD>(v, t0, min(t1, c.C), tid, 256, flags);
+  tree_units_sync();
+#pragma unroll 1
+  for (int x = 0; x < HD; x += TA_EX)
+#pragma unroll 1
+    for (int t = tid; t < pad * 4; t += 256) {
+      const int r = t >> 2;
+      if (r >= c.rows) break;
+      if (!tree_weights_ok(ml, r, pad)) continue;
+      const int row = c.block * TA_BLOCK + r, node = row / G;
+      uint64_t nodes = p.mask[(size_t)c.b * p.c.max_nodes + node];
+      if (c.seq.n < 64) nodes &= (1ull << c.seq.n) - 1;
+      uint16_t* out = p.out + (((size_t)c.b * p.c.max_nodes + node) * p.Hq + c.kvh * G + (row - node * G)) * HD;
+#pragma unroll 1
+      for (int d = x + (t & 3) * 8; d < x + (t & 3) * 8 + 8; ++d) {
+        const float was = part ? part[(size_t)r * HD + d] : bf2f(out[d]);
+        if (fabsf(was) < INFINITY) continue;
+        const float now = flagged_sum(flags[d] | node_flags<HD>(v, t0, t1, c.C, nodes, d), was);
+        if (part) part[(size_t)r * HD + d] = now;
+        else out[d] = f2bf(now);
+      }
+    }
+  tree_units_sync();
 }
 
 template <int HD>
@@ -626,6 +680,7 @@ __device__ void tree_softmax(const TreeDev& p, TreeShared<HD>& sh, unsigned char
     for (int t = c.first_mixed(); t < c.tile1; ++t, ++jobs)
       if (c.both || ((t - c.tile0) & 1) == unit) dirty |= sh.dirty[jobs % TA_JOBS];
     dirty = worked && real ? dirty & nodes : 0ull;
+    bool redo = false;  // any sums that are no numbers
     // 32 columns at a time: every lane leaves its own, then a thread adds up eight columns of a row (the places are turned by the
     // columns' group, so that the four threads of a row read from different banks)
 #pragma unroll 1
@@ -650,6 +705,10 @@ __device__ void tree_softmax(const TreeDev& p, TreeShared<HD>& sh, unsigned char
         for (int i = r; i < 256; i += pad)
 #pragma unroll
           for (int e = 0; e < 8; ++e) a[e] += ex[(col + e) * 256 + (i ^ col)];
+        float none = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) none = fmaf(a[e], 0.f, none);
+        if (none != 0.f) redo = redo || tree_weights_ok(ex_ml, r, pad);
         if (whole) {
           *reinterpret_cast<uint4*>(p.out + q_at(c, block0 + r) + x + col) =
               make_uint4(ta_pack(a[0], a[1]), ta_pack(a[2], a[3]), ta_pack(a[4], a[5]), ta_pack(a[6], a[7]));
@@ -659,8 +718,9 @@ __device__ void tree_softmax(const TreeDev& p, TreeShared<HD>& sh, unsigned char
           dst[1] = make_float4(a[4], a[5], a[6], a[7]);
         }
       }
-      tree_units_sync();
+      redo = tree_units_any(redo);
     }
+    if (redo) tree_redo<HD>(p, c, pad, ex_ml, reinterpret_cast<int*>(ex), whole ? nullptr : p.part.sums + part * HD);
     if (u_next >= u1) break;
     c = next;
     u = u_next;
