@@ -322,6 +322,10 @@ typedef struct sol_tree {
   const uint64_t *mask;   /* device [B][max_nodes]: bit j of node i's word: i attends to node j.  Whatever the caller
                              puts there counts (a chain's lower triangle, a tree's ancestors, a node without itself);
                              bits of nodes that are not there are ignored */
+  int32_t weight_parts;   /* sol_tree_attn, max_nodes * n_q_heads / n_kv_heads above 16: 2: the softmax weights are multiplied with
+                             the values as two bf16 parts, as in the decode step's attention; 1 or 0: rounded to bf16.  (Error of
+                             an output against 64 bits by L2 norm, its own rounding to bf16 included: 0.0017 and 0.0023; two
+                             parts take up to 1.4 times as long.)  Up to 16 it is two parts in any case */
 } sol_tree_t;
 /* Ancestor masks (the node itself among them) and, optionally, depths (a root's is 0) of trees given by their parents:
  * parents[b][i] < i, or -1 for a root; any other value counts as -1.  Rows behind a tree's last node are left as they
@@ -338,7 +342,7 @@ size_t sol_tree_workspace_bytes(const sol_shape_t *shape, int32_t max_batch, int
  * does not see it; neither do slots behind the sequence.  Tokens of a page whose number is out of range are skipped and
  * raise the status bit.  At most 256 kv-heads.
  * A value that is infinite makes its element of every row that sees it infinite, NaN where NaN or the other infinity is seen too.
- * Scores, maxima and sums are float32; the weights are rounded to bf16 for the product with V.
+ * Scores, maxima and sums are float32; the weights in the product with V are bf16, in one part or two (weight_parts).
  *   q_bf16 [B][max_nodes][n_q][head_dim] (already rotated); out_bf16 the same shape. */
 sol_status_t sol_tree_attn(const sol_shape_t *shape, const void *q_bf16, const sol_kv_t *kv, const sol_tree_t *tree, int32_t B,
                            void *out_bf16, void *ws, size_t ws_bytes, sol_stream_t stream);

@@ -46,7 +46,8 @@ class SolKV(C.Structure):
 
 
 class SolTree(C.Structure):
-    _fields_ = [("max_nodes", C.c_int32), ("n_nodes", C.c_void_p), ("mask", C.c_void_p)]
+    _fields_ = [("max_nodes", C.c_int32), ("n_nodes", C.c_void_p), ("mask", C.c_void_p),
+                ("weight_parts", C.c_int32)]
 
 
 class SolKeyOrigin(C.Structure):
@@ -350,9 +351,10 @@ def kv_refresh(shape, layers, kvs, B: int, n_tokens: int, h_in_bf16, h_out_bf16,
 MAX_TREE_NODES = 64
 
 
-def make_tree(max_nodes: int, n_nodes, mask=None) -> SolTree:
-    """Trees of drafted tokens: n_nodes int32 [B], mask 64-bit words [B][max_nodes] (tree_commit needs none)."""
-    return SolTree(max_nodes, _ptr(n_nodes), _ptr(mask))
+def make_tree(max_nodes: int, n_nodes, mask=None, weight_parts: int = 1) -> SolTree:
+    """Trees of drafted tokens: n_nodes int32 [B], mask 64-bit words [B][max_nodes] (tree_commit needs none).  weight_parts 2: the
+    attention carries its weights in two bf16 parts whatever the size."""
+    return SolTree(max_nodes, _ptr(n_nodes), _ptr(mask), weight_parts)
 
 
 def tree_workspace_bytes(shape: SolShape, max_batch: int, max_pages_per_seq: int, max_nodes: int) -> int:

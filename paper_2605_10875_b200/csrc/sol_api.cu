@@ -792,7 +792,9 @@ static bool cache_size_ok(const sol_shape_t* s, const sol_kv_t* kv) {
   return s->n_kv_heads <= 256 && kv->max_pages_per_seq <= MAX_PAGES_PER_SEQ &&
          (long long)kv->num_pages * s->n_kv_heads * PAGE < (1ll << 31);
 }
-static bool tree_ok(const sol_tree_t* t) { return t && t->n_nodes && t->mask && t->max_nodes >= 1; }
+static bool tree_ok(const sol_tree_t* t) {
+  return t && t->n_nodes && t->mask && t->max_nodes >= 1 && (t->weight_parts == 0 || t->weight_parts == 1 || t->weight_parts == 2);
+}
 static bool aligned8(const void* a) { return (reinterpret_cast<uintptr_t>(a) & 7) == 0; }
 // Do n int32 at a share any with the m at b?  (An output that other CTAs of the call still read as an input.)
 static bool share_ints(const void* a, size_t n, const void* b, size_t m) {
@@ -831,7 +833,7 @@ sol_status_t sol_tree_attn(const sol_shape_t* shape, const void* q_bf16, const s
   RowsArgs a;
   memset(&a, 0, sizeof(a));
   a.shape = *shape; a.kv = *kv; a.B = B;
-  a.max_nodes = tree->max_nodes; a.n_nodes = tree->n_nodes; a.mask = tree->mask;
+  a.max_nodes = tree->max_nodes; a.n_nodes = tree->n_nodes; a.mask = tree->mask; a.low_parts = tree->weight_parts == 2;
   a.q = q_bf16; a.out = out_bf16;
   a.part = at<float>(ws, 256); a.part_bytes = ws_bytes - 256;
   a.status = at<int>(ws, 0);

@@ -349,6 +349,7 @@ struct RowsArgs {
   const uint64_t* mask;     // [B][max_nodes]; nullptr: decode steps
   const void* q;            // bf16 [B][max_nodes][Hq][hd]
   void* out;                // same
+  bool low_parts;           // trees of many query rows: the weights' low parts are multiplied with the values too
   float* part;              // scratch for the chains that are cut between CTAs
   size_t part_bytes;
   float* weights;           // optional, decode steps: [B][Hkv][max_pages * 64], updated: decay * old + this step's

@@ -11,7 +11,8 @@
 // softmax uses all four of the SM's quarters.  What the units and the copies have is added up at the end of a piece.
 //
 //   warps 0-3, 4-7   the units' softmax, a lane per thread: scores from tensor memory, running maximum (moved only where it
-//                    grows by more than 2^8: then the sums are rescaled), weights as bf16 back to where the scores were
+//                    grows by more than 2^8: then the sums are rescaled), weights as bf16 (LOW: in two parts) back to where the
+//                    scores were
 //   warps 8, 9       TMA of keys, of values into a ring each of 128-token operand tiles (128-byte swizzle)
 //   warp 10          tcgen05.mma: S = Q K^T (both from shared memory), O += P V (P from tensor memory)
 //   warp 11          clears rows of values that no weight may meet: behind the sequence, and of drafted tokens that are not finite,
@@ -37,6 +38,7 @@ constexpr int ta_piece_cost(int hd) { return hd == 64 ? 8 : 4; }
 constexpr int TA_THREADS = 12 * 32;
 constexpr uint32_t POLL_LIMIT = 1u << 24;  // polls of the products' warp: some tenths of a second
 constexpr float TA_SLACK = 8.f;         // weights reach 2^8 before the maximum moves
+constexpr int TA_LOW = TA_TILE / 2;     // columns from weights' high parts to their low parts, over the tile's scores
 constexpr int TA_EX = 32;               // columns handed over at a time at the end of a piece
 enum : int { TAW_KEYS = 8, TAW_VALUES = 9, TAW_MMA = 10, TAW_CLEAR = 11 };
 
@@ -261,7 +263,7 @@ __device__ void tree_clear(const TreeDev& p, TreeShared<HD>& sh, uint32_t v_ring
 // This warp's pace is the kernel's.  It waits without naps (mbar_test_wait_at) for all that a step needs at once, a barrier per
 // lane, and issues a step's products and commits in one elected block on operands that are the same in all lanes: 32 to 62 cycles
 // a product, where predicated ones took 80 and blocks on lanes' own values more than that.
-template <int HD>
+template <int HD, bool LOW>
 __device__ void tree_mma(const TreeDev& p, TreeShared<HD>& sh, uint32_t q_oper, uint32_t k_ring, uint32_t v_ring, int u0, int u1) {
   using Z = TaSize<HD>;
   constexpr uint32_t S_IDESC = umma_idesc_bf16_m128(TA_TILE, 0, 0), O_IDESC = umma_idesc_bf16_m128(HD, 0, 1);
@@ -310,8 +312,11 @@ __device__ void tree_mma(const TreeDev& p, TreeShared<HD>& sh, uint32_t q_oper, 
     const uint32_t base = tmem + unit * Z::UNIT;
     const uint64_t b = v_desc + (uint64_t)(v_slot * (Z::OPER >> 4));
 #pragma unroll
-    for (int k = half * 4; k < half * 4 + 4; ++k)
-      umma_bf16_ts(base + TA_TILE, base + k * 8, b + (uint64_t)(k * 2048 >> 4), O_IDESC, !fresh || k > 0);
+    for (int k = half * 4; k < half * 4 + 4; ++k) {
+      const uint64_t v = b + (uint64_t)(k * 2048 >> 4);
+      umma_bf16_ts(base + TA_TILE, base + k * 8, v, O_IDESC, !fresh || k > 0);
+      if (LOW) umma_bf16_ts(base + TA_TILE, base + TA_LOW + k * 8, v, O_IDESC, true);
+    }
   };
   auto values_end = [&](int unit, bool last, bool end) {
     if (last) umma_commit(&sh.v_empty[v_slot]);
@@ -433,9 +438,13 @@ __device__ __noinline__ void tree_rescale(uint32_t tm_o, float f) {
 // A tile's W tokens from column `seg` W of the scores on: weights to the front of the scores' columns (the other tokens' are zero).
 // base: the first of these tokens; m, l: running maximum (base 2) and sum; fresh: the unit has no sums yet.  (Its products so far
 // are over: these scores were asked for after them.)  A whole tile's weights are handed over in two halves: the first is multiplied
-// while the second is computed (256 rows of the 8B shape 295 -> 280 us, 48 ragged sequences 169 -> 151).  A quarter of the powers as
-// a cubic on the FMA pipes instead of the special-function unit was slower (289 -> 299, 151 -> 177).
-template <int HD, int W>
+// while the second is computed (in runs too short for the power cap: 256 rows of the 8B shape 295 -> 280 us, 48 ragged sequences 169 ->
+// 151; in long ones the second takes 318 to 338 and 158 to 168).  A quarter of the powers as a cubic on the FMA pipes instead of the
+// special-function unit was slower (289 -> 299, 151 -> 177).
+// The weights are rounded to bf16 for their product, which puts an output off by 0.0023 in all where its own rounding alone makes 0.0017;
+// LOW, the caller's choice, multiplies what the rounding took as well.  It is not the rule because the products then bound even what HBM
+// did: 16 trees of 64 rows 40 -> 47 us, 48 ragged ones 168 -> 229, 256 rows of the 8B shape 338 -> 443, one of 100 rows 47.4 -> 48.4.
+template <int HD, int W, bool LOW>
 __device__ __forceinline__ void tree_step(const TreeDev& p, uint32_t tm_s, int seg, int base, int C, uint64_t nodes, int there,
                                           bool fresh, float& m, float& l, uint64_t* first_half) {
   uint32_t s[W];
@@ -465,30 +474,38 @@ __device__ __forceinline__ void tree_step(const TreeDev& p, uint32_t tm_s, int s
   const float shift = m == -INFINITY ? 0.f : -m;
   const uint64_t scale2 = f32x2(p.scale_log2, p.scale_log2), shift2 = f32x2(shift, shift);
   uint64_t sum[2] = {0, 0};
-  uint32_t w[W / 2];
+  constexpr int N = LOW ? 16 : 32;  // words of a whole tile that are stored at a time
+  uint32_t hi[W / 2], lo[LOW ? W / 2 : 1];
 #pragma unroll
   for (int i = 0; i < W / 2; ++i) {
     const float2 e = ta_unpack2(fma_f32x2(f32x2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), scale2, shift2));
     const float a = ta_exp2(e.x), b = ta_exp2(e.y);
     sum[i & 1] = ta_add2(sum[i & 1], f32x2(a, b));
-    w[i] = ta_pack(a, b);
-    if (W == TA_TILE && i == 31) tmem_st32(tm_s, w);
-    if (W == TA_TILE && i == 35) {  // stored by now
+    hi[i] = ta_pack(a, b);
+    if constexpr (LOW) lo[i] = ta_pack(a - bf16_lo(hi[i]), b - bf16_hi(hi[i]));
+    if (W == TA_TILE && i % N == N - 1) {
+      if constexpr (LOW) {
+        tmem_st16(tm_s + i - (N - 1), hi + i - (N - 1));
+        tmem_st16(tm_s + TA_LOW + i - (N - 1), lo + i - (N - 1));
+      } else {
+        tmem_st32(tm_s + i - (N - 1), hi + i - (N - 1));
+      }
+    }
+    if (W == TA_TILE && i == 35) {  // the first half is stored by now
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
       if (threadIdx.x % 32 == 0) mbar_arrive(first_half);
     }
   }
-  if constexpr (W == TA_TILE) {
-    tmem_st32(tm_s + 32, w + 32);
-  } else {  // seg W / 2 words of zeros, the weights, zeros
+  if constexpr (W != TA_TILE) {  // seg W / 2 words of zeros, the weights, zeros
     uint32_t z[32];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
+    for (int half = 0; half < (LOW ? 4 : 2); ++half) {
 #pragma unroll
-      for (int i = 0; i < 32; ++i) z[i] = seg == (half * 32 + i) / (W / 2) ? w[i % (W / 2)] : 0u;
-      tmem_st32(tm_s + half * 32, z);
+      for (int i = 0; i < 32; ++i)
+        z[i] = seg == ((half & 1) * 32 + i) / (W / 2) ? (LOW && half > 1 ? lo : hi)[i % (W / 2)] : 0u;
+      tmem_st32(tm_s + (half >> 1) * TA_LOW + (half & 1) * 32, z);
     }
   }
   const float2 both = ta_unpack2(ta_add2(sum[0], sum[1]));
@@ -554,7 +571,7 @@ __device__ __noinline__ void tree_redo(const TreeDev& p, const TreePiece c, int 
   tree_units_sync();
 }
 
-template <int HD>
+template <int HD, bool LOW>
 __device__ void tree_softmax(const TreeDev& p, TreeShared<HD>& sh, unsigned char* q_smem, int u0, int u1) {
   using Z = TaSize<HD>;
   constexpr int PPR = HD / 8, STEP = 256 / PPR;  // 16-byte pieces of a row; rows that 256 threads bring at once
@@ -630,9 +647,9 @@ __device__ void tree_softmax(const TreeDev& p, TreeShared<HD>& sh, unsigned char
       wait(&sh.s_full[unit], done & 1);
       tc_fence_after();
       if (warp_real) {
-        if (c.lanes == 128) tree_step<HD, 128>(p, tm_s, 0, base, c.C, nodes, there, j == from, m, l, &sh.p_half[unit]);
-        else if (c.lanes == 64) tree_step<HD, 64>(p, tm_s, seg, base + seg * 64, c.C, nodes, there, j == from, m, l, &sh.p_half[unit]);
-        else tree_step<HD, 32>(p, tm_s, seg, base + seg * 32, c.C, nodes, there, j == from, m, l, &sh.p_half[unit]);
+        if (c.lanes == 128) tree_step<HD, 128, LOW>(p, tm_s, 0, base, c.C, nodes, there, j == from, m, l, &sh.p_half[unit]);
+        else if (c.lanes == 64) tree_step<HD, 64, LOW>(p, tm_s, seg, base + seg * 64, c.C, nodes, there, j == from, m, l, &sh.p_half[unit]);
+        else tree_step<HD, 32, LOW>(p, tm_s, seg, base + seg * 32, c.C, nodes, there, j == from, m, l, &sh.p_half[unit]);
       }
       tc_fence_before();
       __syncwarp();
@@ -727,7 +744,7 @@ __device__ void tree_softmax(const TreeDev& p, TreeShared<HD>& sh, unsigned char
   }
 }
 
-template <int HD>
+template <int HD, bool LOW>
 __global__ void __launch_bounds__(TA_THREADS, 1) tree_attn_kernel(const __grid_constant__ CUtensorMap kmap,
                                                                   const __grid_constant__ CUtensorMap vmap, const __grid_constant__ TreeDev p) {
   using Z = TaSize<HD>;
@@ -768,10 +785,10 @@ __global__ void __launch_bounds__(TA_THREADS, 1) tree_attn_kernel(const __grid_c
   const int u0 = range.x, u1 = range.y;
   if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");  // 168 a thread at launch: 128 threads give 64 each,
   else asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");            // 256 take 32 each
-  if (warp < 8) tree_softmax<HD>(p, sh, q_smem, u0, u1);
+  if (warp < 8) tree_softmax<HD, LOW>(p, sh, q_smem, u0, u1);
   else if (warp == TAW_KEYS) tree_load<HD, false>(p, sh, k_ring, &kmap, u0, u1);
   else if (warp == TAW_VALUES) tree_load<HD, true>(p, sh, v_ring, &vmap, u0, u1);
-  else if (warp == TAW_MMA) tree_mma<HD>(p, sh, smem_u32(q_smem), smem_u32(k_ring), smem_u32(v_ring), u0, u1);
+  else if (warp == TAW_MMA) tree_mma<HD, LOW>(p, sh, smem_u32(q_smem), smem_u32(k_ring), smem_u32(v_ring), u0, u1);
   else {
     if (tid == TAW_CLEAR * 32) chain_describe(p.c, sh.plan, blockIdx.x, u0, u1, p.part.desc);
     __syncwarp();
@@ -785,10 +802,10 @@ __global__ void __launch_bounds__(TA_THREADS, 1) tree_attn_kernel(const __grid_c
 static int tree_rows(const sol_shape_t& sh, int max_nodes) { return std::min(TA_BLOCK, max_nodes * (sh.n_q_heads / sh.n_kv_heads)); }
 size_t tree_part_bytes(const sol_shape_t& sh, int max_nodes) { return chain_part_bytes(sm_count(), tree_rows(sh, max_nodes), sh.head_dim); }
 
-template <int HD>
+template <int HD, bool LOW>
 static void launch_tree(const TreeDev& d, const CUtensorMap& kmap, const CUtensorMap& vmap, int ctas, cudaStream_t st) {
-  ensure_dynamic_smem(reinterpret_cast<const void*>(&tree_attn_kernel<HD>), TaSize<HD>::SMEM);
-  SOL_LAUNCH("tree_attn", tree_attn_kernel<HD>, dim3(ctas), dim3(TA_THREADS), TaSize<HD>::SMEM, st, kmap, vmap, d);
+  ensure_dynamic_smem(reinterpret_cast<const void*>(&tree_attn_kernel<HD, LOW>), TaSize<HD>::SMEM);
+  SOL_LAUNCH("tree_attn", (tree_attn_kernel<HD, LOW>), dim3(ctas), dim3(TA_THREADS), TaSize<HD>::SMEM, st, kmap, vmap, d);
   launch_chain_merge(d.c, d.part, d.Hq, HD, ctas, d.out, st);
 }
 
@@ -807,8 +824,13 @@ void launch_tree_attention(const RowsArgs& a, cudaStream_t st) {
   d.out = static_cast<uint16_t*>(a.out);
   d.part = chain_parts(a.part, ctas, tree_rows(sh, a.max_nodes), sh.head_dim);
   d.status = a.status;
-  if (sh.head_dim == 64) launch_tree<64>(d, kmap, vmap, ctas, st);
-  else launch_tree<128>(d, kmap, vmap, ctas, st);
+  if (sh.head_dim == 64) {
+    if (a.low_parts) launch_tree<64, true>(d, kmap, vmap, ctas, st);
+    else launch_tree<64, false>(d, kmap, vmap, ctas, st);
+  } else {
+    if (a.low_parts) launch_tree<128, true>(d, kmap, vmap, ctas, st);
+    else launch_tree<128, false>(d, kmap, vmap, ctas, st);
+  }
 }
 
 }  // namespace sol

@@ -135,6 +135,14 @@ def test_new_lengths_over_the_path_are_refused():
                (sol.SOL_OK, commit(0x5000, B=0))])
 
 
+def test_weight_parts_are_one_or_two():
+    def call(parts, size=0):
+        return lambda: sol.tree_attn(_shape(), FAKE, _kv(), sol.make_tree(8, FAKE, FAKE, parts), 2, FAKE, FAKE, size, check=False)
+
+    _refusals([(sol.SOL_ERR_INVALID_ARG, call(3)), (sol.SOL_ERR_INVALID_ARG, call(-1))]
+              + [(sol.SOL_ERR_WORKSPACE_TOO_SMALL, call(p)) for p in (0, 1, 2)])
+
+
 def test_tracked_eviction_refuses():
     """What sol_kv_evict refuses, an origin that is not whole, keys without rotation, pools and arrays that overlap."""
     POOL = 32 * 2 * 64 * 64 * 2  # bytes of the cache's keys
