@@ -402,7 +402,8 @@ sol_status_t sol_kv_evict(const sol_shape_t *shape, const sol_kv_t *kv, int32_t 
  *   k_pool: as large as kv->k_pool and with the same pages: the first form of every key that has been moved (the call writes it, and
  *   reads no other rows of it); it must not overlap the cache's pools.
  *   moved int32 [B][n_kv][max_pages_per_seq * page_size]: how far the key in a slot has been moved in all, 0 for one that never was.
- *   dst_moved: the same for the new slots, zeros behind them up to the row's end; it may be moved, and must not overlap it otherwise.
+ *   dst_moved: the same for the new slots, zeros behind them up to the row's end, as if every page were there; it may be moved, and must
+ *   not overlap it otherwise.
  * A sequence begins with zeros in moved.  Keys that are appended to it then need nothing done; who writes a new key into a slot whose
  * entry is not 0 (sol_kv_refresh) sets it to 0.  shape->rope_theta must be above 0: without it keys are not rounded. */
 typedef struct sol_key_origin {
@@ -433,8 +434,9 @@ sol_status_t sol_decode_step_host(const sol_shape_t *shape, int32_t n_layers, co
 /* Device status words of a workspace, copied to HOST out[8] after waiting for
  * `stream`:  out[0] bit mask of errors raised by kernels (bit 0: a bounded
  * wait timed out -> SOL_ERR_DEVICE_TIMEOUT is returned; bit 1: a page-table
- * entry was out of range and the access was skipped; bit 2: a bit-width outside
- * 2..8 and 16 was met and treated as 16), out[1] token
+ * entry was out of range and the access was skipped; bit 2, the bad-action bit: a bit-width
+ * outside 2..8 and 16 was met and treated as 16, or sol_tree_attn or sol_tree_commit met a node count, length
+ * or path out of range and clamped it), out[1] token
  * selections whose near-threshold candidate list overflowed and fell back to
  * float32 ordering, out[2] the same for channel selections, out[3] token
  * candidates re-scored in float64, out[4] channel candidates re-scored. */

@@ -9,7 +9,7 @@ namespace sol {
 
 // ---- device status words (first 256 bytes of every workspace) -------------
 enum : int {
-  ST_ERR = 0,            // bit mask: 1 = bounded wait gave up, 2 = bad page id skipped, 4 = unsupported bit-width
+  ST_ERR = 0,            // bit mask: 1 = bounded wait gave up, 2 = bad page id skipped, 4 = bit-width, node count or path out of range
   ST_TOK_OVERFLOW = 1,   // token selections that fell back to float32 ordering
   ST_CH_OVERFLOW = 2,    // channel selections that fell back
   ST_TOK_REFINED = 3,    // token candidates re-scored in float64
