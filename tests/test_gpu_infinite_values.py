@@ -6,6 +6,7 @@ import torch
 
 from oracle import cache_ops as OC
 from oracle import sol_oracle as O
+from paper_2605_10875_b200 import binding as sol
 from tests import cache_cases as CC
 from tests import harness as H
 from tests.test_gpu_cache_budget import Weighted
@@ -96,3 +97,35 @@ def test_scores_that_are_no_numbers_stay_nan(n):
     c.launch()
     got = O.bf16_to_f64(H.host_u16(c.out))
     assert np.isnan(got[0]).all() and np.isfinite(got[1]).all()
+
+
+@pytest.mark.parametrize("nodes", [0, 1, 24])
+def test_the_longest_pieces(nodes):
+    """The longest contexts, so many of them that a CTA has whole ones: all the values of a piece are looked through, and nobody who waits
+    meanwhile gives up.  (The sequences share their pages, which are only read.)"""
+    cfg = CC.config("g2")
+    shape, _ = H.make_shapes(cfg)
+    B, pages = 128, 768
+    T = pages * 64
+    gen = torch.Generator(device=H.DEV).manual_seed(1)
+    k, v = (torch.empty((pages, 2, 64, 64), dtype=torch.bfloat16, device=H.DEV).normal_(generator=gen) for _ in range(2))
+    v[5, :, 7, 3] = float("inf")
+    v[700, :, 1, 8] = -float("inf")
+    v[701, 0, 1, 8] = float("nan")
+    table = torch.arange(pages, dtype=torch.int32, device=H.DEV).repeat(B, 1)
+    kv = H.DeviceKV(k, v, table, H.dev_i32([T] * B), pages, pages)
+    q = torch.empty((B, max(1, nodes), 4, 64), dtype=torch.bfloat16, device=H.DEV).normal_(generator=gen)
+    out = torch.zeros_like(q)
+    if nodes:
+        mask = torch.full((B, nodes), -1, dtype=torch.int64, device=H.DEV)
+        ws = CC.TreeWorkspace(shape, B, pages, nodes)
+        sol.tree_attn(shape, q, kv.struct(), sol.make_tree(nodes, H.dev_i32([nodes] * B), mask), B, out, ws.buf, ws.bytes)
+    else:
+        ws = H.Workspace(shape, B, pages)
+        weights = torch.zeros((B, 2, T), device=H.DEV)
+        sol.weighted_decode_attn(shape, q, kv.struct(), B, 1.0, weights, out, ws.buf, ws.bytes)
+    assert ws.status()[0] == 0
+    got = out.float()
+    assert torch.isposinf(got[..., 3]).all() and torch.isnan(got[:, :, :2, 8]).all() and torch.isneginf(got[:, :, 2:, 8]).all()
+    rest = [c for c in range(64) if c not in (3, 8)]
+    assert torch.isfinite(got[..., rest]).all()
