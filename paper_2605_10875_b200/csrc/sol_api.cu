@@ -91,10 +91,7 @@ void ensure_dynamic_smem(const void* kernel, int bytes) {
   if (n < 256) table[n++] = Entry{dev, kernel, bytes};
 }
 
-// ---------------------------------------------------------------------------
-// workspace layout
-// ---------------------------------------------------------------------------
-bool encode_pool_map(CUtensorMap* map, const void* pool, const sol_shape_t& sh, int num_pages, int box_rows) {
+bool encode_pool_map(CUtensorMap* map, const void* pool, const sol_shape_t& sh, int num_pages) {
   using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                               const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -113,7 +110,7 @@ bool encode_pool_map(CUtensorMap* map, const void* pool, const sol_shape_t& sh, 
   }
   const cuuint64_t dims[2] = {(cuuint64_t)sh.head_dim, (cuuint64_t)num_pages * sh.n_kv_heads * PAGE};
   const cuuint64_t strides[1] = {(cuuint64_t)sh.head_dim * 2};
-  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, step[2] = {1, 1};
+  const cuuint32_t box[2] = {64, PAGE}, step[2] = {1, 1};
   const CUresult r = reinterpret_cast<Encode>(fn)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(pool), dims, strides,
                                                   box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -122,6 +119,9 @@ bool encode_pool_map(CUtensorMap* map, const void* pool, const sol_shape_t& sh, 
   return false;
 }
 
+// ---------------------------------------------------------------------------
+// workspace layout
+// ---------------------------------------------------------------------------
 struct Layout {
   size_t status, zero_p, stage_h_in, stage_act, stage_h_out, a_op, scale, qkv, attn_hi, attn_lo, attn_f32, h_mid, o_part, g, u, t, t_hi, t_lo, kept_ch_cnt, live, ch_sel, ch_cand_val, ch_cand_idx, ch_keep, down_part,
       h_a, h_b, refresh_tab, refresh_act, total;

@@ -28,6 +28,11 @@ __device__ __forceinline__ float bf2f(uint16_t u) { return __uint_as_float(((uin
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return (uint32_t)f2bf(lo) | ((uint32_t)f2bf(hi) << 16);
 }
+__device__ __forceinline__ uint32_t cvt_bf16x2(float lo, float hi) {  // the same in one instruction
+  uint32_t y;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
+  return y;
+}
 
 // ---- pairs of float32 in one 64-bit register: one instruction multiplies and adds both -------------
 __device__ __forceinline__ uint64_t f32x2(float lo, float hi) {

@@ -226,12 +226,6 @@ __device__ __forceinline__ void em_copy16(uint32_t dst_smem, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst_smem), "l"(src) : "memory");
 }
 
-__device__ __forceinline__ uint32_t em_pack(float lo, float hi) {
-  uint32_t y;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
-  return y;
-}
-
 // TRACK: with tracked origins.  A key that has been moved before comes from its row of first_keys, and every key that moves leaves
 // there what it was, in the same order as the rows themselves: what is read later lies behind every slot written so far, in either pool.
 template <int HD, int READERS, bool TRACK>
@@ -450,8 +444,8 @@ __global__ void __launch_bounds__((2 * READERS + 2) * 32) evict_move_kernel(cons
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const float l0 = bf16_lo(l[2 * q + i]), l1 = bf16_hi(l[2 * q + i]), h0 = bf16_lo(h[2 * q + i]), h1 = bf16_hi(h[2 * q + i]);
-            new_l[2 * q + i] = em_pack(l0 * cs[2 * i] - h0 * sn[2 * i], l1 * cs[2 * i + 1] - h1 * sn[2 * i + 1]);
-            new_h[2 * q + i] = em_pack(h0 * cs[2 * i] + l0 * sn[2 * i], h1 * cs[2 * i + 1] + l1 * sn[2 * i + 1]);
+            new_l[2 * q + i] = cvt_bf16x2(l0 * cs[2 * i] - h0 * sn[2 * i], l1 * cs[2 * i + 1] - h1 * sn[2 * i + 1]);
+            new_h[2 * q + i] = cvt_bf16x2(h0 * cs[2 * i] + l0 * sn[2 * i], h1 * cs[2 * i + 1] + l1 * sn[2 * i + 1]);
           }
         }
         dst[f0] = back ? make_uint4(new_l[0], new_l[1], new_l[2], new_l[3]) : lo;

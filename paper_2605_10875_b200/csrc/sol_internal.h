@@ -363,8 +363,8 @@ void launch_rows_attention(const RowsArgs& a, cudaStream_t st);
 // Trees of many query rows (sol_tree_attn.cu): the same arguments, without weights.
 size_t tree_part_bytes(const sol_shape_t& sh, int max_nodes);
 void launch_tree_attention(const RowsArgs& a, cudaStream_t st);
-// Tensor map of a pool's rows: boxes of 64 elements x box_rows rows, 128-byte swizzle.  False (and a recorded error) if it fails.
-bool encode_pool_map(struct CUtensorMap_st* map, const void* pool, const sol_shape_t& sh, int num_pages, int box_rows);
+// Tensor map of a pool's rows: boxes of 64 elements x a page's rows, 128-byte swizzle.  False (and a recorded error) if it fails.
+bool encode_pool_map(struct CUtensorMap_st* map, const void* pool, const sol_shape_t& sh, int num_pages);
 
 // ---- bookkeeping of drafted trees (sol_tree.cu) ----------------------------
 constexpr int MAX_TREE_NODES = 64;

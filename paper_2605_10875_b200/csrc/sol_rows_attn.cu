@@ -617,8 +617,8 @@ template <int HD, int ROWS>
 static void launch_rows(RowsDev d, const RowsArgs& a, cudaStream_t st) {
   using Z = RaSize<HD, ROWS>;
   CUtensorMap kmap, vmap;
-  if (!encode_pool_map(&kmap, a.kv.k_pool, a.shape, a.kv.num_pages, PAGE) ||
-      !encode_pool_map(&vmap, a.kv.v_pool, a.shape, a.kv.num_pages, PAGE))
+  if (!encode_pool_map(&kmap, a.kv.k_pool, a.shape, a.kv.num_pages) ||
+      !encode_pool_map(&vmap, a.kv.v_pool, a.shape, a.kv.num_pages))
     return;
   // fewer CTAs where the caller's space for partial results is short
   const int rows = std::min(ROWS, d.c.max_nodes * d.c.G);

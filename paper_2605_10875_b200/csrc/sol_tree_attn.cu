@@ -98,11 +98,6 @@ __device__ __forceinline__ float ta_max3(float a, float b, float c) {  // of num
   asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
   return y;
 }
-__device__ __forceinline__ uint32_t ta_pack(float lo, float hi) {
-  uint32_t y;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
-  return y;
-}
 __device__ __forceinline__ uint64_t ta_add2(uint64_t a, uint64_t b) {
   uint64_t y;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
@@ -481,8 +476,8 @@ __device__ __forceinline__ void tree_step(const TreeDev& p, uint32_t tm_s, int s
     const float2 e = ta_unpack2(fma_f32x2(f32x2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), scale2, shift2));
     const float a = ta_exp2(e.x), b = ta_exp2(e.y);
     sum[i & 1] = ta_add2(sum[i & 1], f32x2(a, b));
-    hi[i] = ta_pack(a, b);
-    if constexpr (LOW) lo[i] = ta_pack(a - bf16_lo(hi[i]), b - bf16_hi(hi[i]));
+    hi[i] = cvt_bf16x2(a, b);
+    if constexpr (LOW) lo[i] = cvt_bf16x2(a - bf16_lo(hi[i]), b - bf16_hi(hi[i]));
     if (W == TA_TILE && i % N == N - 1) {
       if constexpr (LOW) {
         tmem_st16(tm_s + i - (N - 1), hi + i - (N - 1));
@@ -728,7 +723,7 @@ __device__ void tree_softmax(const TreeDev& p, TreeShared<HD>& sh, unsigned char
         if (none != 0.f) redo = redo || tree_weights_ok(ex_ml, r, pad);
         if (whole) {
           *reinterpret_cast<uint4*>(p.out + q_at(c, block0 + r) + x + col) =
-              make_uint4(ta_pack(a[0], a[1]), ta_pack(a[2], a[3]), ta_pack(a[4], a[5]), ta_pack(a[6], a[7]));
+              make_uint4(cvt_bf16x2(a[0], a[1]), cvt_bf16x2(a[2], a[3]), cvt_bf16x2(a[4], a[5]), cvt_bf16x2(a[6], a[7]));
         } else {
           float4* dst = reinterpret_cast<float4*>(p.part.sums + (part + r) * HD + x + col);
           dst[0] = make_float4(a[0], a[1], a[2], a[3]);
@@ -812,7 +807,7 @@ static void launch_tree(const TreeDev& d, const CUtensorMap& kmap, const CUtenso
 void launch_tree_attention(const RowsArgs& a, cudaStream_t st) {
   const sol_shape_t& sh = a.shape;
   CUtensorMap kmap, vmap;
-  if (!encode_pool_map(&kmap, a.kv.k_pool, sh, a.kv.num_pages, PAGE) || !encode_pool_map(&vmap, a.kv.v_pool, sh, a.kv.num_pages, PAGE))
+  if (!encode_pool_map(&kmap, a.kv.k_pool, sh, a.kv.num_pages) || !encode_pool_map(&vmap, a.kv.v_pool, sh, a.kv.num_pages))
     return;
   const int ctas = sm_count();
   TreeDev d;
