@@ -201,11 +201,12 @@ __device__ __forceinline__ float2 turn_back(uint32_t back, uint2 speed) {
 // moves back never falls from one row to the next and hardly changes within a chunk, so its angle is put together from two tables
 // in shared memory, of 0 .. 63 positions and of the chunk's few multiples of 64 (an angle from the polynomials for every pair takes
 // three times the instructions); chunks that span more have their angles from the polynomials.
-// Bound by HBM and the time from a chunk's request to its write for batches (half of 24 ragged caches, 1.1 GB: 213 us), by that time
-// and the chunks of the longest sequence otherwise (half of 30000 tokens: 81 us).  Dropped: rows read into registers, between
-// barriers, 4 us a round, 317 us for the first; bulk copies of single rows, 25 to 40 ns each, 1447 us; every writer asking for every
-// chunk itself, 250 ns a chunk, a quarter of 16 sequences of 4096 33 us where it is now 26; seven readers for a CTA that has an SM to
-// itself, 121 us for the second; rotated keys' pieces without their swap, 218 us for the first.
+// Bound by HBM and the time from a chunk's request to its write for batches (half of 24 ragged caches, 1.1 GB: 214 us, and 199 where
+// nothing is rotated), by that time and the chunks of the longest sequence otherwise (half of 30000 tokens: 82 us; a quarter of 16
+// sequences of 4096: 27, 22 without rotation; by events around the kernel, which are some 3 us of each).  Dropped: rows read into
+// registers, between barriers, 4 us a round, 317 us for the first; bulk copies of single rows, 25 to 40 ns each, 1447 us; every
+// writer asking for every chunk itself, 250 ns a chunk, 33 us for the third; seven readers for a CTA that has an SM to itself, 121 us
+// for the second; rotated keys' pieces without their swap, 218 us for the first.
 constexpr int EM_FEW = 7, EM_MANY = 15;  // warps that read: where two CTAs share an SM, where one has it to itself
 constexpr uint32_t EM_POLLS = 1u << 22;  // some tenths of a second
 constexpr int EM_FAR = 4;          // multiples of 64 positions in a chunk's table

@@ -41,7 +41,8 @@ struct RowsDev {
 
 // ROWS query rows per chain: 16, 8 or 4.
 // Bound by HBM: one query token of 64 sequences of 8000 of the 8B shape takes 316 us (2.1 GB, 6.6 TB/s; steps of half a tile, in
-// 4 KB boxes, took 403), with 16 rows 32 sequences take 171 us of which the bytes need 161; at head_dim 64 176 of 161.
+// 4 KB boxes, took 403), with 16 rows 32 sequences take 171 us of which the bytes need 161; at head_dim 64 64 sequences take 175
+// of 161 with up to 8 rows, 204 with 16, where the products of two blocks of rows fill the warps' time.
 template <int HD, int ROWS>
 struct RaSize {
   static constexpr int HALF = PAGE * 128;      // a 64-wide half of the keys: [64 tokens][128 B]
